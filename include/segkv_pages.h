@@ -1,0 +1,131 @@
+/*
+ * segkv_pages — a key/value cache in pages, for serving: requests come and go, each owns the pages that its row of a
+ * block table lists.  Stands beside the segment cache of segkv.h, whose batch begins and ends together: a prompt can be
+ * attended to by segkv_prefill_sdpa and stored here, and a request can go back to a segment cache for beam
+ * search (segkv_pages_read gives its rows in the layout that segkv_prefill_write takes).
+ *
+ * One handle is one attention layer's cache.  The pages themselves are the caller's memory; the handle holds
+ * their geometry, the split workspace of the attention kernel and a device error word.
+ *
+ * Conventions are those of segkv.h (error codes, streams, ownership, one caller at a time per handle: two calls of one
+ * handle that may run at the same time, two captured graphs among them, share its workspace and have to be ordered
+ * by the caller), and:
+ *   - every call has to be made with the handle's device current (EINVAL otherwise);
+ *   - n sequences; table: device int32 [n][table_stride], entry j of a row is the page that holds positions
+ *     [j*page_size, (j+1)*page_size) of that sequence; entries behind a sequence's end are not read;
+ *   - lens: device int32 [n], the length of every sequence COUNTING the tokens of the step at hand, in
+ *     append, attention and read alike: a step raises it once and makes all its calls with it.  A length of 0 is
+ *     an empty slot of a padded batch;
+ *   - what only the device can see is not refused but flagged in the device error word (segkv_pages_get_error):
+ *     SEGKV_DEV_BAD_PAGE: a page id outside the pool, or a length that is negative or longer than the table's row.
+ *       A token whose page is bad or whose position is behind the row is not stored; the read takes page 0 for a
+ *       bad page and leaves out positions behind the row; the attention takes page 0 and clamps the length;
+ *     SEGKV_DEV_BAD_POSITION: a token's position lies behind the rotation tables: it is not stored, nor its query rotated;
+ *   - tokens that would stand before a sequence's start (more of them asked for than it has) do not exist.
+ *
+ * Pages.  K and V pages are two arrays [num_pages][kv_heads][page_size rows].  With kv_bits 16 a row is head_dim values of the
+ * handle's dtype.  With kv_bits 4 the rows of one (page, kv head) are page_size rows of head_dim/2 bytes of codes
+ * (channel d in nibble d%2 of byte d/2), then page_size rows of eight 16-bit values of the handle's dtype: scales
+ * s[0..3] and zero points z[0..3] of the row's four groups; channel d belongs to group d%4 and stands for
+ * z + s*(code - 8).  (Interleaved groups, so that a tensor-core fragment made of a row's consecutive bytes
+ * can be cut by group.)  A group's values x are held by
+ *     step = (max x - min x)/15,  s = r(step),  z = r(min x + 8*step),  code = clamp(rint((x - z)/s) + 8, 0, 15)
+ * (8 where s is 0; r rounds to the dtype, the rest is fp32), an error of about s/2.  A group with an Inf or NaN has s and
+ * z NaN: all of it reads as NaN.
+ */
+#ifndef SEGKV_PAGES_H
+#define SEGKV_PAGES_H
+
+#include "segkv.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef struct segkv_pages* segkv_pages_t;
+
+/* bits of the device error word returned by segkv_pages_get_error, with those of segkv.h */
+enum {
+    SEGKV_DEV_BAD_PAGE = 4,
+    SEGKV_DEV_BAD_POSITION = 8
+};
+
+/* Bytes of the K pages (and of the V pages).  0 on a bad argument.  Pure host arithmetic. */
+SEGKV_API size_t segkv_pages_bytes(int kv_heads, int head_dim, int page_size, int num_pages, int kv_bits);
+
+/*
+ * A cache over the caller's pages k_pages and v_pages (device memory of segkv_pages_bytes() bytes each on the current
+ * device, 16-byte aligned, which must outlive the handle; their contents are the caller's).  Allocates the
+ * workspace: nothing is allocated later.
+ * Requirements: heads % kv_heads == 0, head_dim in {64, 128, 256}, page_size in {16, 32, 64, 128, 256},
+ * num_pages * kv_heads * page_size < 2^31, dtype SEGKV_F16/BF16, kv_bits 16 or 4.
+ * Errors: EINVAL, ENOMEM, ECUDA.  *out is set only on success.
+ */
+SEGKV_API int segkv_pages_create(segkv_pages_t* out, int heads, int kv_heads, int head_dim, int page_size, int num_pages,
+                                 int dtype, int kv_bits, void* k_pages, void* v_pages);
+
+/* Free what the handle owns (not the pages).  Synchronises the device.  NULL is allowed. */
+SEGKV_API int segkv_pages_destroy(segkv_pages_t h);
+
+/*
+ * Store the newest tokens of n sequences, in one launch, with the position rotation applied on the way.
+ *   k, v: device; token i < tokens of sequence s is row s*tokens + i, kv_heads * head_dim contiguous values, rows k_stride
+ *     (v_stride) elements apart (multiples of 8, at least kv_heads*head_dim): slices of a packed projection will do;
+ *   new_lens: device int32 [n], how many of a sequence's rows are tokens (clamped to [0, tokens]; the rows behind
+ *     them are padding, which may hold anything), or NULL: all `tokens` of them.  Token i goes to position
+ *     lens[s] - new_lens[s] + i;
+ *   rope_cos, rope_sin: device float [rope_positions][head_dim/2] and style as for segkv_append_rope, or NULL: K as it comes.
+ *     A pair (a, b) becomes (a cos - b sin, b cos + a sin), products and sums rounded to fp32, then once to the dtype;
+ *   q, q_out: the queries of the same tokens, heads * head_dim values a row, rows q_stride elements apart, rotated
+ *     like K into q_out [n][tokens][heads][head_dim], contiguous (it may be q itself where that is contiguous); rows
+ *     of q_out without a token are left as they are.  Both NULL: no queries.  Only with a rotation: EINVAL otherwise.
+ * Two tokens of one call that land in the same row of a page leave either's values.
+ * n or tokens 0: nothing to do.  Errors: EINVAL, ECUDA.
+ */
+SEGKV_API int segkv_pages_append(segkv_pages_t h, int n, int tokens, const void* k, long long k_stride, const void* v,
+                                 long long v_stride, const int32_t* table, int table_stride, const int32_t* lens,
+                                 const int32_t* new_lens, const void* q, long long q_stride, void* q_out,
+                                 const float* rope_cos, const float* rope_sin, int rope_positions, int style, void* stream);
+
+/*
+ * Attention of the newest q_len tokens of n sequences over their pages (their own rows included: append first).  Row i
+ * of sequence s stands at position m = lens[s] - q_len + i and
+ *     out[s,i,hd,:] = softmax_{j<=m}(q[s,i,hd,:] . K[s,j,:] / sqrt(head_dim) + slope[hd]*(j - m)) . V[s,j,:]
+ * with K and V the values that the pages stand for; rows with m < 0 are zeros.  q_len is 1 for a decode step, more for
+ * drafts and for a piece of a prompt.
+ *   q: device, rows (s*q_len + i) of heads * head_dim contiguous values, q_stride elements apart (a multiple of 8);
+ *   out: device [n][q_len][heads][head_dim], contiguous;
+ *   alibi_slopes: device float [heads] or NULL.
+ * fp16/bf16 (or 4-bit) operands, fp32 scores, softmax and accumulation, one rounding of the output; the same inputs give
+ * the same bits.  The work is shared out on the device by the sequences' real lengths, so a captured call follows them.
+ * A value row that is not finite reaches the rows that see it; with q_len > 1 it can also reach earlier rows of the
+ * same sequence, whose weight for it is zero (0 * Inf is NaN).  Rows of a page behind a sequence's end reach nothing.
+ * n or q_len 0: nothing to do.  Errors: EINVAL, ECUDA.
+ */
+SEGKV_API int segkv_pages_sdpa(segkv_pages_t h, int n, int q_len, const void* q, long long q_stride, void* out,
+                               const int32_t* table, int table_stride, const int32_t* lens, const float* alibi_slopes,
+                               void* stream);
+
+/*
+ * The mirror of the append: the values that the newest tokens' rows stand for, rounded to the dtype.  k_out, v_out
+ * [n][tokens][kv_heads][head_dim], contiguous; row i < new_lens[s] (NULL: tokens) of sequence s is position
+ * lens[s] - new_lens[s] + i, rows behind them and rows before the sequence's start are left as they are.  new_lens = lens
+ * reads whole sequences, in the layout that segkv_prefill_write_ragged takes.
+ * n or tokens 0: nothing to do.  Errors: EINVAL, ECUDA.
+ */
+SEGKV_API int segkv_pages_read(segkv_pages_t h, int n, int tokens, void* k_out, void* v_out, const int32_t* table,
+                               int table_stride, const int32_t* lens, const int32_t* new_lens, void* stream);
+
+/* Programmatic dependent launch between the library's kernels on a stream (on by default), as segkv_set_overlap. */
+SEGKV_API int segkv_pages_set_overlap(segkv_pages_t h, int enable);
+
+/* Read and clear the device error word (SEGKV_DEV_* bits).  Synchronises the device. */
+SEGKV_API int segkv_pages_get_error(segkv_pages_t h, int* device_flags);
+
+/* Kernels launched by the handle since creation. */
+SEGKV_API long long segkv_pages_launch_count(segkv_pages_t h);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* SEGKV_PAGES_H */

@@ -5,7 +5,7 @@
 
 #include <new>
 
-#include "segkv_internal.h"
+#include "segkv_pages_internal.h"
 
 using namespace segkv_impl;
 
@@ -26,11 +26,12 @@ int cuda_fail(cudaError_t e, const char* what) {
 
 StreamLog g_log;
 
-// The stream of a launch for handle h.
-StreamKey stream_key(const segkv* h, cudaStream_t st) {
+// The stream of a launch on a device; of a launch for handle h.
+StreamKey stream_key(int device, cudaStream_t st) {
     static thread_local char own;
-    return {h->device, st, st == cudaStreamPerThread ? &own : nullptr};
+    return {device, st, st == cudaStreamPerThread ? &own : nullptr};
 }
+StreamKey stream_key(const segkv* h, cudaStream_t st) { return stream_key(h->device, st); }
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -526,6 +527,12 @@ SdpaArgs sdpa_args(const segkv* h, const void* q, void* out, const float* slopes
 }
 
 }  // namespace
+
+namespace segkv_impl {
+// for the paged cache (segkv_pages_api.cu): errors in the library's manner, launches in the order of its streams
+int report_cuda(cudaError_t e, const char* what) { return cuda_fail(e, what); }
+void log_launch(int device, cudaStream_t st, Release rel) { g_log.note(stream_key(device, st), rel); }
+}  // namespace segkv_impl
 
 extern "C" {
 

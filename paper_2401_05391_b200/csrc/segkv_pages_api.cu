@@ -1,0 +1,169 @@
+// Host side of the paged cache: handle life cycle, argument checks, launches.
+#include <string.h>
+
+#include <new>
+
+#include "segkv_pages_internal.h"
+
+using namespace segkv_impl;
+
+namespace {
+
+inline bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+bool geometry_ok(int kv_heads, int head_dim, int page_size, int num_pages, int kv_bits) {
+    if (kv_heads <= 0 || num_pages <= 0) return false;
+    if (head_dim != 64 && head_dim != 128 && head_dim != 256) return false;
+    if (page_size < 16 || page_size > 256 || (page_size & (page_size - 1))) return false;
+    if (kv_bits != 16 && kv_bits != 4) return false;
+    return (double)num_pages * kv_heads * page_size < 2147483648.0;
+}
+
+// The part of the arguments that every call has.
+int check_call(const segkv_pages* h, int n, int tokens, const int32_t* table, int table_stride, const int32_t* lens) {
+    if (!h || n < 0 || tokens < 0) return SEGKV_EINVAL;
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return report_cuda(e, "cudaGetDevice");
+    if (dev != h->device) return SEGKV_EINVAL;
+    if (n == 0 || tokens == 0) return SEGKV_OK;
+    if (!table || !lens || table_stride <= 0 || !aligned(table, 4) || !aligned(lens, 4)) return SEGKV_EINVAL;
+    if ((long long)n * tokens > 0x7FFFFFFFLL) return SEGKV_EINVAL;
+    return SEGKV_OK;
+}
+
+bool rows_ok(const void* p, long long stride, long long width) {
+    return p && aligned(p, 16) && stride >= width && stride % 8 == 0 && stride <= (1LL << 40);
+}
+
+int launched(segkv_pages* h, cudaError_t e, const char* what, void* stream) {
+    if (e != cudaSuccess) return report_cuda(e, what);
+    h->launches++;
+    log_launch(h->device, (cudaStream_t)stream, kAfterWait);
+    return SEGKV_OK;
+}
+
+void free_all(segkv_pages* h) {
+    void* ptrs[] = {h->ws, h->tickets, h->err_word};
+    for (void* p : ptrs)
+        if (p) cudaFree(p);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t segkv_pages_bytes(int kv_heads, int head_dim, int page_size, int num_pages, int kv_bits) {
+    if (!geometry_ok(kv_heads, head_dim, page_size, num_pages, kv_bits)) return 0;
+    return (size_t)num_pages * kv_heads * page_size * page_row_bytes(head_dim, kv_bits);
+}
+
+int segkv_pages_create(segkv_pages_t* out, int heads, int kv_heads, int head_dim, int page_size, int num_pages, int dtype,
+                       int kv_bits, void* k_pages, void* v_pages) {
+    if (!out || !geometry_ok(kv_heads, head_dim, page_size, num_pages, kv_bits)) return SEGKV_EINVAL;
+    if (heads <= 0 || heads % kv_heads || (dtype != SEGKV_F16 && dtype != SEGKV_BF16)) return SEGKV_EINVAL;
+    if (!k_pages || !v_pages || !aligned(k_pages, 16) || !aligned(v_pages, 16)) return SEGKV_EINVAL;
+    segkv_pages* h = new (std::nothrow) segkv_pages();
+    if (!h) return SEGKV_ENOMEM;
+    memset(h, 0, sizeof *h);
+    h->heads = heads; h->kv_heads = kv_heads; h->group = heads / kv_heads; h->head_dim = head_dim;
+    h->page_size = page_size; h->num_pages = num_pages; h->dtype = dtype; h->bits = kv_bits;
+    while ((1 << h->page_log) < page_size) h->page_log++;
+    h->overlap = true;
+    h->kp = (char*)k_pages;
+    h->vp = (char*)v_pages;
+#define SEGKV_TRY(call)                          \
+    do {                                         \
+        cudaError_t e__ = (call);                \
+        if (e__ != cudaSuccess) {                \
+            const int rc__ = report_cuda(e__, #call); \
+            free_all(h);                         \
+            delete h;                            \
+            return rc__;                         \
+        }                                        \
+    } while (0)
+    SEGKV_TRY(cudaGetDevice(&h->device));
+    SEGKV_TRY(cudaDeviceGetAttribute(&h->sm_count, cudaDevAttrMultiProcessorCount, h->device));
+    const size_t grid = (size_t)pages_sdpa_grid(*h);
+    SEGKV_TRY(cudaMalloc((void**)&h->ws, grid * 2 * pages_sdpa_slot_floats(*h) * sizeof(float)));
+    SEGKV_TRY(cudaMalloc((void**)&h->tickets, grid * sizeof(int)));
+    SEGKV_TRY(cudaMalloc((void**)&h->err_word, sizeof(int)));
+    SEGKV_TRY(cudaMemset(h->tickets, 0, grid * sizeof(int)));
+    SEGKV_TRY(cudaMemset(h->err_word, 0, sizeof(int)));
+#undef SEGKV_TRY
+    *out = h;
+    return SEGKV_OK;
+}
+
+int segkv_pages_destroy(segkv_pages_t h) {
+    if (!h) return SEGKV_OK;
+    cudaDeviceSynchronize();
+    free_all(h);
+    delete h;
+    return SEGKV_OK;
+}
+
+int segkv_pages_append(segkv_pages_t h, int n, int tokens, const void* k, long long k_stride, const void* v, long long v_stride,
+                       const int32_t* table, int table_stride, const int32_t* lens, const int32_t* new_lens, const void* q,
+                       long long q_stride, void* q_out, const float* rope_cos, const float* rope_sin, int rope_positions,
+                       int style, void* stream) {
+    const int rc = check_call(h, n, tokens, table, table_stride, lens);
+    if (rc != SEGKV_OK || n == 0 || tokens == 0) return rc;
+    const long long kw = (long long)h->kv_heads * h->head_dim, qw = (long long)h->heads * h->head_dim;
+    if (!rows_ok(k, k_stride, kw) || !rows_ok(v, v_stride, kw) || !aligned(new_lens, 4)) return SEGKV_EINVAL;
+    const bool rope = rope_cos || rope_sin;
+    if (rope) {
+        if (!rope_cos || !rope_sin || !aligned(rope_cos, 4) || !aligned(rope_sin, 4) || rope_positions <= 0) return SEGKV_EINVAL;
+        if (style != SEGKV_ROPE_HALF && style != SEGKV_ROPE_INTERLEAVED) return SEGKV_EINVAL;
+    }
+    if (q || q_out) {
+        if (!rope || !rows_ok(q, q_stride, qw) || !q_out || !aligned(q_out, 16)) return SEGKV_EINVAL;
+        if (q == q_out && q_stride != qw) return SEGKV_EINVAL;
+    }
+    PageAppendArgs a;
+    a.t = {n, tokens, table, table_stride, lens, new_lens, h->overlap};
+    a.k = k; a.v = v; a.q = q;
+    a.k_stride = k_stride; a.v_stride = v_stride; a.q_stride = q_stride;
+    a.q_out = q_out;
+    a.cos = rope_cos; a.sin = rope_sin;
+    a.positions = rope_positions;
+    a.style = rope ? style : 0;
+    return launched(h, launch_pages_append(*h, a, (cudaStream_t)stream), "segkv_pages_append", stream);
+}
+
+int segkv_pages_sdpa(segkv_pages_t h, int n, int q_len, const void* q, long long q_stride, void* out, const int32_t* table,
+                     int table_stride, const int32_t* lens, const float* alibi_slopes, void* stream) {
+    const int rc = check_call(h, n, q_len, table, table_stride, lens);
+    if (rc != SEGKV_OK || n == 0 || q_len == 0) return rc;
+    if (!rows_ok(q, q_stride, (long long)h->heads * h->head_dim) || !out || !aligned(out, 16) || !aligned(alibi_slopes, 4)) return SEGKV_EINVAL;
+    if ((long long)n * q_len * h->group > 0x7FFFFFFFLL) return SEGKV_EINVAL;
+    PageSdpaArgs a = {n, q_len, q, q_stride, out, table, table_stride, lens, alibi_slopes, h->overlap};
+    return launched(h, launch_pages_sdpa(*h, a, (cudaStream_t)stream), "segkv_pages_sdpa", stream);
+}
+
+int segkv_pages_read(segkv_pages_t h, int n, int tokens, void* k_out, void* v_out, const int32_t* table, int table_stride,
+                     const int32_t* lens, const int32_t* new_lens, void* stream) {
+    const int rc = check_call(h, n, tokens, table, table_stride, lens);
+    if (rc != SEGKV_OK || n == 0 || tokens == 0) return rc;
+    if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16) || !aligned(new_lens, 4)) return SEGKV_EINVAL;
+    const PageTokens t = {n, tokens, table, table_stride, lens, new_lens, h->overlap};
+    return launched(h, launch_pages_read(*h, t, k_out, v_out, (cudaStream_t)stream), "segkv_pages_read", stream);
+}
+
+int segkv_pages_set_overlap(segkv_pages_t h, int enable) {
+    if (!h) return SEGKV_EINVAL;
+    h->overlap = enable != 0;
+    return SEGKV_OK;
+}
+
+int segkv_pages_get_error(segkv_pages_t h, int* device_flags) {
+    if (!h || !device_flags) return SEGKV_EINVAL;
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemcpy(device_flags, h->err_word, sizeof(int), cudaMemcpyDeviceToHost);
+    if (e == cudaSuccess) e = cudaMemset(h->err_word, 0, sizeof(int));
+    return e == cudaSuccess ? SEGKV_OK : report_cuda(e, "segkv_pages_get_error");
+}
+
+long long segkv_pages_launch_count(segkv_pages_t h) { return h ? h->launches : (long long)SEGKV_EINVAL; }
+
+}  // extern "C"

@@ -1,0 +1,74 @@
+// Internal declarations of the paged cache (host API and kernels).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "segkv_internal.h"
+#include "segkv_pages.h"
+
+struct segkv_pages {
+    int device, sm_count;
+    int heads, kv_heads, group, head_dim, page_size, page_log, num_pages, dtype, bits;
+    bool overlap;
+    long long launches;
+    char *kp, *vp;       // the caller's pages
+    float* ws;           // partial results of work groups that several CTAs share: two slots per CTA
+    int* tickets;        // [CTAs] arrival counters, zero between launches
+    int* err_word;
+};
+
+namespace segkv_impl {
+
+// bytes of one key or value row in its page, scales included
+inline size_t page_row_bytes(int head_dim, int bits) { return bits == 16 ? (size_t)head_dim * 2 : (size_t)head_dim / 2 + 16; }
+
+struct PageTokens {              // arguments that append and read share
+    int n, tokens;
+    const int32_t* table;
+    int table_stride;
+    const int32_t *lens, *new_lens;
+    bool pdl;
+};
+
+struct PageAppendArgs {
+    PageTokens t;
+    const void *k, *v, *q;
+    long long k_stride, v_stride, q_stride;
+    void* q_out;
+    const float *cos, *sin;
+    int positions, style;        // style 0: K as it comes
+};
+
+struct PageSdpaArgs {
+    int n, q_len;
+    const void* q;
+    long long q_stride;
+    void* out;
+    const int32_t* table;
+    int table_stride;
+    const int32_t* lens;
+    const float* slopes;
+    bool pdl;
+};
+
+cudaError_t launch_pages_append(const segkv_pages& h, const PageAppendArgs& a, cudaStream_t st);
+cudaError_t launch_pages_read(const segkv_pages& h, const PageTokens& t, void* k_out, void* v_out, cudaStream_t st);
+cudaError_t launch_pages_sdpa(const segkv_pages& h, const PageSdpaArgs& a, cudaStream_t st);
+int pages_sdpa_grid(const segkv_pages& h);                  // most CTAs of an attention launch
+size_t pages_sdpa_slot_floats(const segkv_pages& h);        // floats of one CTA's partial result
+
+// What the position and page of a token come to.
+__device__ __forceinline__ int clamped_len(int len, int most, int* err) {
+    if (len < 0 || len > most) {
+        atomicOr(err, SEGKV_DEV_BAD_PAGE);
+        return len < 0 ? 0 : most;
+    }
+    return len;
+}
+
+// launches of the library outside segkv_api.cu: errors in its manner, order on its streams
+int report_cuda(cudaError_t e, const char* what);
+void log_launch(int device, cudaStream_t st, Release rel);
+
+}  // namespace segkv_impl

@@ -1,0 +1,882 @@
+// Attention of the newest tokens of a batch of sequences over their pages, rows held in 16 or in 4 bits.
+//
+// Work.  A work group is one (sequence, tile of query columns, kv head): the q_len * group query rows that read the same keys,
+// 8 or 16 at a time.  Its keys are cut into blocks of four warps' tiles, and the blocks of all work groups, in
+// order, are dealt evenly over a resident grid: every CTA takes one contiguous run of blocks, whatever the lengths
+// are, which only the device knows.  A CTA's run begins and ends inside a work group at most; those two write partial
+// results (maximum, sum, weighted values), and the last CTA to arrive at a work group's counter folds its parts in
+// their order, so that the result does not depend on who is last.
+//
+// Warps work alone: each copies its own tiles (cp.async, a ring of kStages), scores them with the keys on the M side
+// (S^T[16 keys, 8 columns] = K . Q^T, mma.sync, fp32), keeps its own running reference and sum, and adds
+// O^T[16 channels, 8 columns] += V^T . P^T.  They meet at the end of a work group only.  A page holds 16 or more rows of one head
+// side by side, so a 16-key tile is one contiguous piece.
+#include <atomic>
+
+#include "segkv_pages_internal.h"
+#include "segkv_ptx.cuh"
+
+namespace segkv_impl {
+namespace {
+
+using namespace ptx;
+
+constexpr int kWarps = 4, kThreads = 32 * kWarps, kStages = 3;
+constexpr float kLog2e = 1.4426950408889634f;
+// A column's weights are taken relative to a reference that is only moved when a score exceeds it by 2^kSlack.
+constexpr float kSlack = 8.f;
+
+struct Params {
+    const char* q;
+    long long q_stride;              // bytes
+    char* out;
+    const char *kp, *vp;
+    const int32_t *table, *lens;
+    const float* slopes;
+    float* ws;
+    int* tickets;
+    int* err;
+    int table_stride, n, q_len, H, Hkv, group, page_log, num_pages;
+    int cols, ctiles;                // query columns of a (sequence, kv head), tiles of them
+};
+
+template <typename T> struct Num;
+template <> struct Num<__half> {
+    static constexpr uint32_t kMagic = 0x64006400u;          // 1024 in both halves: a code in the low bits adds itself
+    static constexpr float kMagicValue = 1024.f;
+    static constexpr uint32_t kMagicPlus8 = 0x64086408u;     // 1032
+    static constexpr float kLift = 6.f;                      // weights carry 2^kLift, so that small ones stay normal
+    static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t b) {
+        const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+        return *reinterpret_cast<const uint32_t*>(&r);
+    }
+    static __device__ __forceinline__ void mma8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
+        asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(b0));
+    }
+};
+template <> struct Num<__nv_bfloat16> {
+    static constexpr uint32_t kMagic = 0x43004300u;          // 128
+    static constexpr float kMagicValue = 128.f;
+    static constexpr uint32_t kMagicPlus8 = 0x43084308u;     // 136
+    static constexpr float kLift = 0.f;
+    static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t b) {
+        const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+        return *reinterpret_cast<const uint32_t*>(&r);
+    }
+    static __device__ __forceinline__ void mma8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
+        asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(b0));
+    }
+};
+
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+    uint32_t r;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r) : "r"(a));
+    return r;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t a) {
+    uint16_t r;
+    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(r) : "r"(a));
+    return r;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+    uint2 r;
+    asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(a));
+    return r;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+    uint4 r;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(a));
+    return r;
+}
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool real) {     // zeros where it is not
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0));
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Shared-memory shape of a variant.  NT: tiles of eight query columns; a warp's tile is SUB pieces of 16 keys.
+template <int D, int NT, int BITS> struct Shape {
+    static constexpr int SUB = BITS == 16 ? (D == 64 ? 2 : 1) : (D == 256 ? 1 : 2);
+    static constexpr int TK = 16 * SUB, KB = kWarps * TK;
+    static constexpr int RB = BITS == 16 ? 2 * D : D / 2;                     // bytes of a row without its scales
+    static constexpr int VOFF = TK * RB, SOFF = 2 * TK * RB;
+    static constexpr int STAGE = 2 * TK * (RB + (BITS == 4 ? 16 : 0));
+    static constexpr int NC = 8 * NT;
+    static constexpr int RING = kWarps * kStages * STAGE;
+    static constexpr int MERGE = kWarps * 8 * 68 * 4;                         // 64 channels of eight columns of every warp
+    static constexpr int ML = kWarps * NC * 2 * 4;
+    static constexpr int SMEM = RING + MERGE + ML + 64;
+    static constexpr int CTAS = BITS == 16 ? (D == 256 ? 1 : 2) : (D == 256 ? 2 : 3);
+    static constexpr int MT = D / 16;                                         // 16-channel tiles of the output
+    static constexpr int SLOT = NC * (D + 2);
+};
+
+// Where 16-byte chunk c of row k (0..15) of a 16-row piece lies: 4-bit rows, whose readers take a row's bytes by fours of lanes and
+// four rows at a time: without bank conflicts for rows (0, 4), (1, 5), .. read by eight lanes and for rows 0..3 read by 16.
+template <int D> __device__ __forceinline__ uint32_t code_at(int k, int c) {
+    if (D == 64) return (k >> 2) * 128 + ((((k & 3) * 2 + c) ^ (((k >> 2) & 1) * 4)) * 16);
+    if (D == 128) return (k >> 1) * 128 + ((((k & 1) * 4 + c) ^ ((((k >> 1) & 1) << 1) | (((k >> 2) & 1) << 2))) * 16);
+    return k * 128 + ((c ^ (((k & 3) << 1) ^ (((k >> 2) & 1) << 2))) * 16);
+}
+
+struct Cursor {                      // a block of keys in the grid's order
+    int v, h, b, nb, klen;
+};
+
+// Keys that column tile ct of sequence s reads, and how many blocks that makes (at least one: an empty sequence's output is written too).
+template <int NC, int KB>
+__device__ __forceinline__ void extent(const Params& p, int v, int* klen, int* nb, bool flag) {
+    const int s = v / p.ctiles, ct = v - s * p.ctiles;
+    const int most = (int)min((long long)p.table_stride << p.page_log, 0x7FFFFFFFLL);
+    int len = __ldg(p.lens + s);
+    if (len < 0 || len > most) {
+        if (flag) atomicOr(p.err, SEGKV_DEV_BAD_PAGE);
+        len = len < 0 ? 0 : most;
+    }
+    const int last = min(p.cols, (ct + 1) * NC) - 1;
+    int k = len - p.q_len + last / p.group + 1;
+    k = k < 0 ? 0 : k;
+    *klen = k;
+    *nb = k > KB ? (k + KB - 1) / KB : 1;
+}
+
+template <int NC, int KB>
+__device__ __forceinline__ void advance(const Params& p, Cursor& c, int V) {
+    if (++c.b < c.nb) return;
+    c.b = 0;
+    if (++c.h < p.Hkv) return;
+    c.h = 0;
+    if (++c.v < V) extent<NC, KB>(p, c.v, &c.klen, &c.nb, false);
+}
+
+template <typename T, int D, int NT, int BITS>
+__global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa_kernel(const __grid_constant__ Params p) {
+    using Sh = Shape<D, NT, BITS>;
+    using M = Mma<T>;
+    using N = Num<T>;
+    constexpr int NC = Sh::NC, KB = Sh::KB, TK = Sh::TK, SUB = Sh::SUB, MT = Sh::MT, RB = Sh::RB;
+    constexpr int W = D / 32;                                 // 4 bits: code words of a key row that a lane scores
+    constexpr int QJ = D / 16;                                // k-steps of a score
+    extern __shared__ __align__(128) char smem[];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    float* s_merge = reinterpret_cast<float*>(smem + Sh::RING);
+    float* s_ml = reinterpret_cast<float*>(smem + Sh::RING + Sh::MERGE);      // [warp][column]{reference, sum}
+    int* s_misc = reinterpret_cast<int*>(smem + Sh::RING + Sh::MERGE + Sh::ML);
+    const uint32_t ring = smem_u32(smem) + warp * (kStages * Sh::STAGE);
+
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    // ---- this CTA's run of blocks -------------------------------------------------------------------------------------------
+    const int V = p.n * p.ctiles;
+    const int per = (V + kThreads - 1) / kThreads;
+    int G = gridDim.x;
+    const int cta = blockIdx.x;
+    unsigned long long x0, x1, total;
+    Cursor ld;
+    {
+        long long* s_scan = reinterpret_cast<long long*>(s_merge);
+        long long mine = 0;
+        const int v0 = min(tid * per, V), v1 = min(v0 + per, V);
+        int klen, nb;
+        for (int v = v0; v < v1; ++v) {
+            extent<NC, KB>(p, v, &klen, &nb, cta == 0);
+            mine += nb;
+        }
+        long long incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long u = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += u;
+        }
+        if (lane == 31) s_scan[warp] = incl;
+        __syncthreads();
+        long long before = incl - mine, all = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) before += s_scan[w];
+            all += s_scan[w];
+        }
+        total = (unsigned long long)all * p.Hkv;
+        if (total < (unsigned long long)G) G = (int)total;    // every CTA of a shared work group has to have a part
+        if (cta >= G) return;                                 // (every thread)
+        x0 = total * cta / G;
+        x1 = total * (cta + 1) / G;
+        unsigned long long at = (unsigned long long)before * p.Hkv;
+        if (mine > 0 && x0 >= at && x0 < at + (unsigned long long)mine * p.Hkv) {
+            for (int v = v0;; ++v) {
+                extent<NC, KB>(p, v, &klen, &nb, false);
+                const unsigned long long size = (unsigned long long)nb * p.Hkv;
+                if (x0 < at + size) {
+                    const unsigned rest = (unsigned)(x0 - at);
+                    s_misc[0] = v;
+                    s_misc[1] = (int)(rest / (unsigned)nb);
+                    s_misc[2] = (int)(rest % (unsigned)nb);
+                    break;
+                }
+                at += size;
+            }
+        }
+        __syncthreads();
+        ld.v = s_misc[0];
+        ld.h = s_misc[1];
+        ld.b = s_misc[2];
+        extent<NC, KB>(p, ld.v, &ld.klen, &ld.nb, false);
+    }
+    Cursor cur = ld;
+    const int blocks = (int)(x1 - x0);
+
+    // ---- copies -------------------------------------------------------------------------------------------------------------
+    int pid[SUB];                                             // pages of the next tile to be copied
+    auto find_pages = [&](const Cursor& c) {
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            const int key = c.b * KB + warp * TK + 16 * u;
+            pid[u] = 0;
+            if (key < c.klen) pid[u] = __ldg(p.table + (long long)(c.v / p.ctiles) * p.table_stride + (key >> p.page_log));
+        }
+    };
+    auto copy_tile = [&](const Cursor& c, int stage) {
+        const uint32_t dst = ring + stage * Sh::STAGE;
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            const int key = c.b * KB + warp * TK + 16 * u;
+            if (key >= c.klen) continue;
+            int page = pid[u];
+            if ((unsigned)page >= (unsigned)p.num_pages) {
+                if (lane == 0) atomicOr(p.err, SEGKV_DEV_BAD_PAGE);
+                page = 0;
+            }
+            const int off = key & ((1 << p.page_log) - 1), left = c.klen - key;          // rows of the piece that exist
+            const size_t slab = ((size_t)page * p.Hkv + c.h) << p.page_log;              // row of the pool
+            if (BITS == 16) {
+                constexpr int CH = RB / 16;                   // chunks of a row
+                const size_t at = (slab + off) * RB;
+#pragma unroll
+                for (int i = 0; i < 16 * CH / 32; ++i) {
+                    const int k = (i * 32 + lane) / CH, ch = (i * 32 + lane) % CH;
+                    const uint32_t to = dst + u * 16 * RB + k * RB + ((ch ^ (k & 7)) * 16);
+                    const size_t from = at + (size_t)(i * 32 + lane) * 16;
+                    cp16(to, p.kp + from, k < left);
+                    cp16(to + Sh::VOFF, p.vp + from, k < left);
+                }
+            } else {
+                constexpr int CH = RB / 16;
+                const int ps = 1 << p.page_log;
+                const size_t blk = slab * (RB + 16), at = blk + (size_t)off * RB;
+#pragma unroll
+                for (int i = 0; i < (16 * CH + 31) / 32; ++i) {
+                    const int idx = i * 32 + lane;
+                    const uint32_t to = dst + u * 16 * RB + code_at<D>(idx / CH, idx % CH);
+                    cp16(to, p.kp + at + idx * 16, true);
+                    cp16(to + Sh::VOFF, p.vp + at + idx * 16, true);
+                }
+                // scales: lanes 0-15 the keys', 16-31 the values'; rows that do not exist get zeros and stand for 0
+                const char* base = lane < 16 ? p.kp : p.vp;
+                cp16(dst + Sh::SOFF + (lane < 16 ? 0 : TK * 16) + (u * 16 + (lane & 15)) * 16,
+                     base + blk + (size_t)ps * RB + (off + (lane & 15)) * 16, (lane & 15) < left);
+            }
+        }
+        cp_commit();
+    };
+
+    int copied = 0;
+    find_pages(ld);
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) {
+        if (copied < blocks) {
+            copy_tile(ld, i);
+            ++copied;
+            if (copied < blocks) {
+                advance<NC, KB>(p, ld, V);
+                find_pages(ld);
+            }
+        } else {
+            cp_commit();
+        }
+    }
+    int stage = 0, fill = kStages - 1;
+
+    // lane constants of the 4-bit form: rows kappa(g) and kappa(g) + 8 of a piece are M rows g and g + 8 of the scores, which makes
+    // M rows 2x, 2x + 1 (+ 8) keys x, x + 4 (+ 8): the pairs a lane needs of V
+    const int kap = (g >> 1) + 4 * (g & 1);
+    const int key_lo = BITS == 16 ? g : kap;
+
+    const float scale2 = kLog2e / sqrtf((float)D);
+    uint32_t qf[NT][QJ][2];
+    float cinit[BITS == 4 ? NT : 1][4][2];                    // 4 bits: what the magic number adds to a group's sum
+    uint32_t qsum[BITS == 4 ? NT : 1];                        // 4 bits: the groups' sums of q, in two parts (B operand)
+    int lim[NT][2];
+    float slope2[NT][2];
+    float mref[NT][2], lsum[NT][2];
+    float o[NT][MT][4];
+    float zo[BITS == 4 ? NT : 1][4];
+    int vexp = -1;                                            // 4 bits, fp16: exponent that the values' scales are taken relative to
+
+    unsigned long long x = x0;
+    for (int done = 0; done < blocks;) {
+        // ---- a work group, or this CTA's part of it ----------------------------------------------------------------------------
+        const int s = cur.v / p.ctiles, ct = cur.v - s * p.ctiles;
+        const int count = min(cur.nb - cur.b, blocks - done);
+        const bool whole = count == cur.nb;
+        const int first_row = ct * NC / p.group;
+        const int last_row = (min(p.cols, (ct + 1) * NC) - 1) / p.group;
+        const int pos0 = cur.klen - 1 - last_row;             // position of row 0; below 0 where the sequence is shorter than q_len
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int col = ct * NC + nt * 8 + g;
+            const bool real = col < p.cols;
+            const int row = real ? col / p.group : 0, hq = cur.h * p.group + (real ? col - row * p.group : 0);
+            const char* qr = p.q + ((long long)s * p.q_len + row) * p.q_stride + (size_t)hq * (2 * D);
+            if (BITS == 16) {
+#pragma unroll
+                for (int j = 0; j < QJ; ++j) {
+                    qf[nt][j][0] = real ? __ldg(reinterpret_cast<const uint32_t*>(qr + (16 * j + 2 * t) * 2)) : 0u;
+                    qf[nt][j][1] = real ? __ldg(reinterpret_cast<const uint32_t*>(qr + (16 * j + 8 + 2 * t) * 2)) : 0u;
+                }
+            } else {
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    const int d = D == 256 ? (w < 4 ? 32 * t + 8 * w : 128 + 32 * t + 8 * (w - 4)) : (8 * W * t + 8 * w);
+                    uint4 r = make_uint4(0u, 0u, 0u, 0u);
+                    if (real) r = __ldg(reinterpret_cast<const uint4*>(qr + d * 2));
+                    const uint32_t pr[4] = {__byte_perm(r.x, r.z, 0x5410), __byte_perm(r.x, r.z, 0x7632),
+                                            __byte_perm(r.y, r.w, 0x5410), __byte_perm(r.y, r.w, 0x7632)};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {             // group j: channels j and j + 4 of the eight
+                        qf[nt][j * (W / 2) + (w >> 1)][w & 1] = pr[j];
+                        const float2 f = M::unpack(pr[j]);
+                        sum[j] += f.x + f.y;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 1);
+                    sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 2);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        cinit[nt][j][e] = -(N::kMagicValue + 8.f) * __shfl_sync(0xffffffffu, sum[j], (2 * t + e) * 4);
+                }
+                // (2^-7: sums of 64 values of fp16 stay finite)
+                const float a = (t & 1 ? sum[2] : sum[0]) * 0.0078125f, b = (t & 1 ? sum[3] : sum[1]) * 0.0078125f;
+                const uint32_t hi = M::pack(a, b);
+                const float2 hf = M::unpack(hi);
+                qsum[nt] = t < 2 ? hi : M::pack(a - hf.x, b - hf.y);
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int c2 = ct * NC + nt * 8 + 2 * t + e;
+                const bool r2 = c2 < p.cols;
+                const int row2 = r2 ? c2 / p.group : first_row;
+                lim[nt][e] = pos0 + row2 + 1;
+                slope2[nt][e] = p.slopes && r2 ? __ldg(p.slopes + cur.h * p.group + (c2 - row2 * p.group)) * kLog2e : 0.f;
+                mref[nt][e] = -INFINITY;
+                lsum[nt][e] = 0.f;
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[nt][m][e] = 0.f;
+            if (BITS == 4)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) zo[nt][e] = 0.f;
+        }
+        const int free_to = pos0 + first_row + 1;             // keys below it are seen by every row of the tile
+        vexp = -1;
+
+        for (int blk = 0; blk < count; ++blk) {
+            const int key0 = (cur.b + blk) * KB + warp * TK;
+            cp_wait<kStages - 2>();
+            __syncwarp();
+            if (key0 < cur.klen) {
+                const uint32_t src = ring + stage * Sh::STAGE;
+                float c[SUB][NT][4];
+                // ---- scores ----------------------------------------------------------------------------------------------------
+#pragma unroll
+                for (int u = 0; u < SUB; ++u) {
+                    if (BITS == 16) {
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) c[u][nt][e] = 0.f;
+                        const int k = lane & 15;
+                        const uint32_t rowp = src + u * 16 * RB + k * RB;
+#pragma unroll
+                        for (int j = 0; j < QJ; ++j) {
+                            uint32_t a[4];
+                            ldmatrix_x4(a, rowp + (((2 * j + (lane >> 4)) ^ (k & 7)) * 16));
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) M::run(c[u][nt], a, qf[nt][j][0], qf[nt][j][1]);
+                        }
+                    } else {
+                        const uint32_t base = src + u * 16 * RB;
+                        uint32_t wl[W], wh[W];
+                        if constexpr (D == 64) {
+                            const uint32_t at = base + code_at<D>(kap, t >> 1) + (t & 1) * 8;
+                            const uint2 a = lds64(at), b = lds64(at + 8 * RB);
+                            wl[0] = a.x; wl[1] = a.y;
+                            wh[0] = b.x; wh[1] = b.y;
+                        } else {
+#pragma unroll
+                            for (int q4 = 0; q4 < W / 4; ++q4) {
+                                const uint32_t at = base + code_at<D>(kap, t + 4 * q4);
+                                const uint4 a = lds128(at), b = lds128(at + 8 * RB);
+                                wl[4 * q4] = a.x; wl[4 * q4 + 1] = a.y; wl[4 * q4 + 2] = a.z; wl[4 * q4 + 3] = a.w;
+                                wh[4 * q4] = b.x; wh[4 * q4 + 1] = b.y; wh[4 * q4 + 2] = b.z; wh[4 * q4 + 3] = b.w;
+                            }
+                        }
+                        const uint32_t sc = src + Sh::SOFF + (u * 16 + kap) * 16;
+                        const uint2 sl = lds64(sc), sh = lds64(sc + 128);
+                        const float2 sl0 = M::unpack(sl.x), sl1 = M::unpack(sl.y), sh0 = M::unpack(sh.x), sh1 = M::unpack(sh.y);
+                        const float fl[4] = {sl0.x, sl0.y, sl1.x, sl1.y}, fh[4] = {sh0.x, sh0.y, sh1.x, sh1.y};
+                        // zero points: sum over groups of z * (sum of q in the group)
+                        const uint32_t za = lds32(sc + 8 + (t & 1) * 4), zb = lds32(sc + 128 + 8 + (t & 1) * 4);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            float z[4] = {0.f, 0.f, 0.f, 0.f};
+                            N::mma8(z, za, zb, qsum[nt]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) c[u][nt][e] = 128.f * z[e];
+                        }
+                        // codes: magic + code from the low bits, group by group, the magic's share taken off by the start value
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            float acc[NT][4];
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                acc[nt][0] = acc[nt][2] = cinit[nt][j][0];
+                                acc[nt][1] = acc[nt][3] = cinit[nt][j][1];
+                            }
+#pragma unroll
+                            for (int w2 = 0; w2 < W / 2; ++w2) {
+                                const uint32_t a[4] = {((wl[2 * w2] >> (4 * j)) & 0x000F000Fu) | N::kMagic, ((wh[2 * w2] >> (4 * j)) & 0x000F000Fu) | N::kMagic,
+                                                       ((wl[2 * w2 + 1] >> (4 * j)) & 0x000F000Fu) | N::kMagic, ((wh[2 * w2 + 1] >> (4 * j)) & 0x000F000Fu) | N::kMagic};
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) M::run(acc[nt], a, qf[nt][j * (W / 2) + w2][0], qf[nt][j * (W / 2) + w2][1]);
+                            }
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                c[u][nt][0] = fmaf(fl[j], acc[nt][0], c[u][nt][0]);
+                                c[u][nt][1] = fmaf(fl[j], acc[nt][1], c[u][nt][1]);
+                                c[u][nt][2] = fmaf(fh[j], acc[nt][2], c[u][nt][2]);
+                                c[u][nt][3] = fmaf(fh[j], acc[nt][3], c[u][nt][3]);
+                            }
+                        }
+                    }
+                }
+                // ---- scale, bias, mask, reference ---------------------------------------------------------------------------------
+                const bool masked = key0 + TK > free_to;
+                bool grow = false;
+#pragma unroll
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float v = c[u][nt][e] * scale2;
+                            const int key = key0 + 16 * u + key_lo + (e >= 2 ? 8 : 0);
+                            if (p.slopes) v = fmaf(slope2[nt][e & 1], (float)(key + 1 - lim[nt][e & 1]), v);
+                            if (masked && key >= lim[nt][e & 1]) v = -INFINITY;
+                            c[u][nt][e] = v;
+                            grow |= v > mref[nt][e & 1] + kSlack;
+                        }
+                if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float mx = mref[nt][e];
+#pragma unroll
+                            for (int u = 0; u < SUB; ++u) mx = fmaxf(mx, fmaxf(c[u][nt][e], c[u][nt][e + 2]));
+                            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                            const float al = mref[nt][e] == -INFINITY ? 0.f : exp2f(mref[nt][e] - mx);
+                            mref[nt][e] = mx;
+                            lsum[nt][e] *= al;
+#pragma unroll
+                            for (int m = 0; m < MT; ++m) {
+                                o[nt][m][e] *= al;
+                                o[nt][m][e + 2] *= al;
+                            }
+                            if (BITS == 4) {
+                                zo[nt][e] *= al;
+                                zo[nt][e + 2] *= al;
+                            }
+                        }
+                }
+                // ---- weights and values -------------------------------------------------------------------------------------------
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float base = mref[nt][e] == -INFINITY ? 0.f : mref[nt][e] - N::kLift;
+#pragma unroll
+                        for (int u = 0; u < SUB; ++u) {
+                            c[u][nt][e] = exp2f(c[u][nt][e] - base);
+                            c[u][nt][e + 2] = exp2f(c[u][nt][e + 2] - base);
+                            lsum[nt][e] += c[u][nt][e] + c[u][nt][e + 2];
+                        }
+                    }
+#pragma unroll
+                for (int u = 0; u < SUB; ++u) {
+                    if (u > 0 && key0 + 16 * u >= cur.klen) break;                     // (nothing was copied there)
+                    if (BITS == 16) {
+                        uint32_t pf[NT][2];
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            pf[nt][0] = movmatrix_trans(M::pack(c[u][nt][0], c[u][nt][1]));
+                            pf[nt][1] = movmatrix_trans(M::pack(c[u][nt][2], c[u][nt][3]));
+                        }
+                        const int k = (lane & 7) + ((lane >> 4) << 3);
+                        const uint32_t rowp = src + Sh::VOFF + u * 16 * RB + k * RB;
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) {
+                            uint32_t a[4];
+                            ldmatrix_x4_trans(a, rowp + (((2 * m + ((lane >> 3) & 1)) ^ (k & 7)) * 16));
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) M::run(o[nt][m], a, pf[nt][0], pf[nt][1]);
+                        }
+                    } else {
+                        const uint32_t sc = src + Sh::SOFF + TK * 16 + u * 256;
+                        // the values' scales go into the weights, in fp32 before their one rounding; the codes stay exact.  fp16 weights
+                        // times a scale would leave the type's range at either end, so scales are taken relative to a power of two
+                        const uint2 sl = lds64(sc + kap * 16), sh = lds64(sc + kap * 16 + 128);
+                        float unit = 1.f;
+                        if (N::kLift > 0.f) {
+                            uint32_t big = __vmaxu2(__vmaxu2(sl.x & 0x7FFF7FFFu, sl.y & 0x7FFF7FFFu), __vmaxu2(sh.x & 0x7FFF7FFFu, sh.y & 0x7FFF7FFFu));
+                            big = max(big & 0xFFFFu, big >> 16) >> 10;
+                            const int top = (int)__reduce_max_sync(0xffffffffu, min(big, 30u));
+                            if (top > vexp) {
+                                if (vexp >= 0) {
+                                    const float down = __int_as_float((127 + vexp - top) << 23);
+#pragma unroll
+                                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                        for (int m = 0; m < MT; ++m)
+#pragma unroll
+                                            for (int e = 0; e < 4; ++e) o[nt][m][e] *= down;
+                                }
+                                vexp = top;
+                            }
+                            unit = __int_as_float((127 + 15 - vexp) << 23);
+                        }
+                        const float2 sl0 = M::unpack(sl.x), sl1 = M::unpack(sl.y), sh0 = M::unpack(sh.x), sh1 = M::unpack(sh.y);
+                        const float fl[4] = {sl0.x * unit, sl0.y * unit, sl1.x * unit, sl1.y * unit};
+                        const float fh[4] = {sh0.x * unit, sh0.y * unit, sh1.x * unit, sh1.y * unit};
+                        uint32_t pf[NT][4][2];
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                pf[nt][j][0] = movmatrix_trans(M::pack(c[u][nt][0] * fl[j], c[u][nt][1] * fl[j]));
+                                pf[nt][j][1] = movmatrix_trans(M::pack(c[u][nt][2] * fh[j], c[u][nt][3] * fh[j]));
+                            }
+                        // zero points: rows 0-3 of one more product are the groups'
+                        {
+                            uint32_t a[4] = {0u, 0u, 0u, 0u};
+                            if (g < 4) {
+                                const uint32_t zp = sc + 8 + 2 * g + t * 16;
+                                a[0] = lds16(zp) | (lds16(zp + 64) << 16);
+                                a[2] = lds16(zp + 128) | (lds16(zp + 192) << 16);
+                            }
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+                                M::run(zo[nt], a, movmatrix_trans(M::pack(c[u][nt][0], c[u][nt][1])), movmatrix_trans(M::pack(c[u][nt][2], c[u][nt][3])));
+                        }
+                        constexpr int VW = D / 64;            // code words of a value row that a lane weighs: channels g*D/8 + 8w ..
+                        uint32_t w4[4][VW];
+                        const uint32_t base = src + Sh::VOFF + u * 16 * RB;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {         // keys t, t + 4, t + 8, t + 12
+                            if constexpr (D == 64) {
+                                w4[i][0] = lds32(base + code_at<D>(t + 4 * (i & 1), g >> 2) + (g & 3) * 4 + (i >> 1) * 8 * RB);
+                            } else if constexpr (D == 128) {
+                                const uint2 r = lds64(base + code_at<D>(t + 4 * (i & 1), g >> 1) + (g & 1) * 8 + (i >> 1) * 8 * RB);
+                                w4[i][0] = r.x; w4[i][1] = r.y;
+                            } else {
+                                const uint4 r = lds128(base + code_at<D>(t + 4 * (i & 1), g) + (i >> 1) * 8 * RB);
+                                w4[i][0] = r.x; w4[i][1] = r.y; w4[i][2] = r.z; w4[i][3] = r.w;
+                            }
+                        }
+#pragma unroll
+                        for (int w = 0; w < VW; ++w) {
+                            // keys t and t + 4 (t + 8 and t + 12) side by side: channels 0-3, then 4-7, of the word's eight
+                            const uint32_t al = __byte_perm(w4[0][w], w4[1][w], 0x5410), ah = __byte_perm(w4[0][w], w4[1][w], 0x7632);
+                            const uint32_t bl = __byte_perm(w4[2][w], w4[3][w], 0x5410), bh = __byte_perm(w4[2][w], w4[3][w], 0x7632);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const uint32_t a[4] = {N::sub(((al >> (4 * j)) & 0x000F000Fu) | N::kMagic, N::kMagicPlus8),
+                                                       N::sub(((ah >> (4 * j)) & 0x000F000Fu) | N::kMagic, N::kMagicPlus8),
+                                                       N::sub(((bl >> (4 * j)) & 0x000F000Fu) | N::kMagic, N::kMagicPlus8),
+                                                       N::sub(((bh >> (4 * j)) & 0x000F000Fu) | N::kMagic, N::kMagicPlus8)};
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) M::run(o[nt][w * 4 + j], a, pf[nt][j][0], pf[nt][j][1]);
+                            }
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+            // ---- the next copy, into the stage of the tile before this one ----------------------------------------------------------
+            if (copied < blocks) {
+                copy_tile(ld, fill);
+                ++copied;
+                if (copied < blocks) {
+                    advance<NC, KB>(p, ld, V);
+                    find_pages(ld);
+                }
+            } else {
+                cp_commit();
+            }
+            stage = stage + 1 == kStages ? 0 : stage + 1;
+            fill = fill + 1 == kStages ? 0 : fill + 1;
+        }
+
+        // ---- the work group's end: warps meet ------------------------------------------------------------------------------------
+        if (BITS == 4) {                                      // zero points' part onto every channel of its group; units undone
+            const float up = vexp >= 0 ? __int_as_float((127 + vexp - 15) << 23) : 1.f;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float zg[4][2];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) zg[j][e] = __shfl_sync(0xffffffffu, zo[nt][e], j * 4 + t);
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[nt][m][e] = fmaf(o[nt][m][e], N::kLift > 0.f ? up : 1.f, zg[m & 3][e & 1]);
+            }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float l = lsum[nt][e];
+                l += __shfl_xor_sync(0xffffffffu, l, 4);
+                l += __shfl_xor_sync(0xffffffffu, l, 8);
+                l += __shfl_xor_sync(0xffffffffu, l, 16);
+                if (g == 0) {
+                    float* ml = s_ml + (warp * NC + nt * 8 + 2 * t + e) * 2;
+                    ml[0] = mref[nt][e];
+                    ml[1] = l;
+                }
+            }
+        __syncthreads();
+        // which CTAs share the work group: the one where it begins uses its second slot, the others their first
+        unsigned long long gbase = x - (unsigned)cur.b;       // (x is the index of block cur.b)
+        const int c0 = whole ? cta : (int)(((gbase + 1) * G - 1) / total);
+        const int c1 = whole ? cta : (int)(((gbase + cur.nb) * G - 1) / total);
+        float* slot = p.ws + ((size_t)cta * 2 + (cta == c0 ? 1 : 0)) * Sh::SLOT;
+        const int mcol = tid >> 4, mloc = (tid & 15) * 4;     // this thread's column (of eight) and channels (of 64) in each round
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) top[e] = fmaxf(top[e], s_ml[(w * NC + nt * 8 + 2 * t + e) * 2]);
+            float f[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) f[e] = mref[nt][e] == -INFINITY ? 1.f : exp2f(mref[nt][e] - top[e]);     // (no weight: zeros, or NaN)
+            float mtop = -INFINITY, lall = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) mtop = fmaxf(mtop, s_ml[(w * NC + nt * 8 + mcol) * 2]);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float mw = s_ml[(w * NC + nt * 8 + mcol) * 2], lw = s_ml[(w * NC + nt * 8 + mcol) * 2 + 1];
+                lall += mw == -INFINITY ? lw : lw * exp2f(mw - mtop);
+            }
+            const int col = ct * NC + nt * 8 + mcol;
+            const int row = col / p.group, hq = cur.h * p.group + (col - row * p.group);
+            const float inv = lall == 0.f ? 0.f : 1.f / lall;
+#pragma unroll
+            for (int r = 0; r < D / 64; ++r) {
+                float* mine = s_merge + warp * (8 * 68);
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int loc = BITS == 16 ? 16 * m + g + (e >= 2 ? 8 : 0) : 8 * g + m + (e >= 2 ? 4 : 0);
+                        mine[(2 * t + (e & 1)) * 68 + loc] = o[nt][r * 4 + m][e] * f[e & 1];
+                    }
+                __syncthreads();
+                float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) {
+                    const float4 b = *reinterpret_cast<const float4*>(s_merge + w * (8 * 68) + mcol * 68 + mloc);
+                    a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+                }
+                const int d = BITS == 16 ? 64 * r + mloc : (mloc >> 3) * (D / 8) + 8 * r + (mloc & 7);
+                if (whole) {
+                    if (col < p.cols) {
+                        uint2 w2;
+                        w2.x = M::pack(a.x * inv, a.y * inv);
+                        w2.y = M::pack(a.z * inv, a.w * inv);
+                        *reinterpret_cast<uint2*>(p.out + ((((size_t)s * p.q_len + row) * p.H + hq) * D + d) * 2) = w2;
+                    }
+                } else {
+                    *reinterpret_cast<float4*>(slot + (nt * 8 + mcol) * D + d) = a;
+                }
+                __syncthreads();
+            }
+            if (!whole && (tid & 15) == 0) {
+                slot[NC * D + nt * 8 + mcol] = mtop;
+                slot[NC * D + NC + nt * 8 + mcol] = lall;
+            }
+        }
+        if (!whole) {
+            // ---- partial results: the last CTA of the work group folds them -------------------------------------------------------
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) s_misc[3] = atomicAdd(p.tickets + c0, 1);
+            __syncthreads();
+            if (s_misc[3] == c1 - c0) {
+                __threadfence();
+                if (tid == 0) p.tickets[c0] = 0;              // as the next launch expects it
+                const int parts = c1 - c0 + 1;
+                auto part = [&](int i) { return p.ws + ((size_t)(c0 + i) * 2 + (i == 0 ? 1 : 0)) * Sh::SLOT; };
+                constexpr int PG = kThreads / NC;             // threads of a column
+                const int fcol = tid % NC, fp = tid / NC;
+                float* s_top = s_merge;                       // [PG][NC], then [NC]
+                float* s_sum = s_merge + kThreads;
+                float* s_f = s_merge + 2 * kThreads;          // [32][NC]
+                float mx = -INFINITY;
+                for (int i = fp; i < parts; i += PG) mx = fmaxf(mx, __ldcg(part(i) + NC * D + fcol));
+                s_top[tid] = mx;
+                __syncthreads();
+                mx = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < PG; ++i) mx = fmaxf(mx, s_top[i * NC + fcol]);
+                float sum = 0.f;
+                for (int i = fp; i < parts; i += PG) {
+                    const float m = __ldcg(part(i) + NC * D + fcol), l = __ldcg(part(i) + NC * D + NC + fcol);
+                    sum += m == -INFINITY ? l : l * exp2f(m - mx);
+                }
+                s_sum[tid] = sum;
+                float4 acc[NT][D / 64];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int r = 0; r < D / 64; ++r) acc[nt][r] = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int i0 = 0; i0 < parts; i0 += 32) {
+                    __syncthreads();
+                    for (int i = fp; i < 32 && i0 + i < parts; i += PG) {
+                        const float m = __ldcg(part(i0 + i) + NC * D + fcol);
+                        s_f[i * NC + fcol] = m == -INFINITY ? 1.f : exp2f(m - mx);     // (no weight: its values are zeros, or NaN)
+                    }
+                    __syncthreads();
+                    const int n = min(32, parts - i0);
+#pragma unroll 4
+                    for (int i = 0; i < n; ++i) {
+                        const float* src = part(i0 + i);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            const float fi = s_f[i * NC + nt * 8 + mcol];
+#pragma unroll
+                            for (int r = 0; r < D / 64; ++r) {
+                                const int d = 64 * r + mloc;
+                                const float4 b = __ldcg(reinterpret_cast<const float4*>(src + (nt * 8 + mcol) * D + d));
+                                acc[nt][r].x = fmaf(b.x, fi, acc[nt][r].x);
+                                acc[nt][r].y = fmaf(b.y, fi, acc[nt][r].y);
+                                acc[nt][r].z = fmaf(b.z, fi, acc[nt][r].z);
+                                acc[nt][r].w = fmaf(b.w, fi, acc[nt][r].w);
+                            }
+                        }
+                    }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const int col = ct * NC + nt * 8 + mcol;
+                    float l = 0.f;
+#pragma unroll
+                    for (int i = 0; i < PG; ++i) l += s_sum[i * NC + nt * 8 + mcol];
+                    const float inv = l == 0.f ? 0.f : 1.f / l;
+                    if (col < p.cols) {
+                        const int row = col / p.group, hq = cur.h * p.group + (col - row * p.group);
+#pragma unroll
+                        for (int r = 0; r < D / 64; ++r) {
+                            uint2 w2;
+                            w2.x = M::pack(acc[nt][r].x * inv, acc[nt][r].y * inv);
+                            w2.y = M::pack(acc[nt][r].z * inv, acc[nt][r].w * inv);
+                            *reinterpret_cast<uint2*>(p.out + ((((size_t)s * p.q_len + row) * p.H + hq) * D + 64 * r + mloc) * 2) = w2;
+                        }
+                    }
+                }
+                __syncthreads();                              // s_merge is the next work group's
+            }
+        }
+        done += count;
+        x += (unsigned)count;
+        cur.b += count - 1;
+        if (done < blocks) advance<NC, KB>(p, cur, V);
+    }
+    cp_wait<0>();
+}
+
+template <typename T, int D, int NT, int BITS>
+cudaError_t launch_variant(const Params& p, int grid, bool pdl, cudaStream_t st) {
+    using Sh = Shape<D, NT, BITS>;
+    static_assert((Sh::SMEM + 1024) * Sh::CTAS <= 233472, "shared memory of the CTAs of an SM");
+    auto kernel = pages_sdpa_kernel<T, D, NT, BITS>;
+    static std::atomic<bool> configured[64] = {};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (dev < 0 || dev >= 64 || !configured[dev].load(std::memory_order_acquire)) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::SMEM);
+        if (e != cudaSuccess) return e;
+        if (dev >= 0 && dev < 64) configured[dev].store(true, std::memory_order_release);
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid, 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = Sh::SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    if (pdl) {
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+    }
+    return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+
+int ctas_per_sm(int D, int bits) { return bits == 16 ? (D == 256 ? 1 : 2) : (D == 256 ? 2 : 3); }
+
+// Columns of a tile: 8, or 16 where there are more; at head_dim 256 always 8 (16 would not fit the registers).
+int columns_of(int D, int cols) { return D == 256 || cols <= 8 ? 8 : 16; }
+
+template <typename T, int BITS>
+cudaError_t launch_typed(int D, int nc, const Params& p, int grid, bool pdl, cudaStream_t st) {
+    if (D == 64) return nc == 8 ? launch_variant<T, 64, 1, BITS>(p, grid, pdl, st) : launch_variant<T, 64, 2, BITS>(p, grid, pdl, st);
+    if (D == 128) return nc == 8 ? launch_variant<T, 128, 1, BITS>(p, grid, pdl, st) : launch_variant<T, 128, 2, BITS>(p, grid, pdl, st);
+    return launch_variant<T, 256, 1, BITS>(p, grid, pdl, st);
+}
+
+}  // namespace
+
+int pages_sdpa_grid(const segkv_pages& h) { return h.sm_count * ctas_per_sm(h.head_dim, h.bits); }
+size_t pages_sdpa_slot_floats(const segkv_pages& h) { return (size_t)(h.head_dim == 256 ? 8 : 16) * (h.head_dim + 2); }
+
+cudaError_t launch_pages_sdpa(const segkv_pages& h, const PageSdpaArgs& a, cudaStream_t st) {
+    Params p;
+    p.q = (const char*)a.q; p.q_stride = a.q_stride * 2; p.out = (char*)a.out;
+    p.kp = h.kp; p.vp = h.vp; p.table = a.table; p.lens = a.lens; p.slopes = a.slopes;
+    p.ws = h.ws; p.tickets = h.tickets; p.err = h.err_word;
+    p.table_stride = a.table_stride; p.n = a.n; p.q_len = a.q_len; p.H = h.heads; p.Hkv = h.kv_heads; p.group = h.group;
+    p.page_log = h.page_log; p.num_pages = h.num_pages;
+    p.cols = a.q_len * h.group;
+    const int nc = columns_of(h.head_dim, p.cols);
+    p.ctiles = (p.cols + nc - 1) / nc;
+    const int grid = pages_sdpa_grid(h);
+    if (h.dtype == SEGKV_BF16)
+        return h.bits == 16 ? launch_typed<__nv_bfloat16, 16>(h.head_dim, nc, p, grid, a.pdl, st) : launch_typed<__nv_bfloat16, 4>(h.head_dim, nc, p, grid, a.pdl, st);
+    return h.bits == 16 ? launch_typed<__half, 16>(h.head_dim, nc, p, grid, a.pdl, st) : launch_typed<__half, 4>(h.head_dim, nc, p, grid, a.pdl, st);
+}
+
+}  // namespace segkv_impl

@@ -1,0 +1,201 @@
+"""Thin binding of the paged cache (``include/segkv_pages.h``): keys and values of requests that come and go, in pages of 16 or 4 bits.
+
+Argument marshalling only, as in :mod:`.segkv`; every step runs in the library's CUDA kernels.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+import torch
+
+from .segkv import SEGKV_BF16, SEGKV_F16, _check, _int, _stream_ptr, _vp, lib
+
+
+def page_bytes(kv_heads: int, head_dim: int, page_size: int, num_pages: int, kv_bits: int = 16) -> int:
+    """Bytes of the K pages (and of the V pages); 0 for a geometry that there is not."""
+    return int(lib().segkv_pages_bytes(kv_heads, head_dim, page_size, num_pages, kv_bits))
+
+
+class PagedKV:
+    """One attention layer's paged cache; methods mirror the C entry points.
+
+    k_pages, v_pages: the pool, CUDA tensors that the handle keeps alive: with kv_bits 16 ``[num_pages, kv_heads, page_size,
+    head_dim]`` of ``dtype``, with kv_bits 4 ``[num_pages, kv_heads, page_size*(head_dim/2 + 16)]`` uint8; None allocates them
+    (zeros) on the current device.  ``table`` [n, entries], ``lens`` [n] and ``new_lens`` [n] are int32 tensors on the
+    pool's device; lens counts the tokens of the step at hand in every call.
+    """
+
+    ROPE_STYLES = {"half": 1, "interleaved": 2}
+
+    def __init__(self, heads: int, kv_heads: int, head_dim: int, page_size: int, num_pages: int, dtype=torch.float16, kv_bits: int = 16,
+                 k_pages: Optional[torch.Tensor] = None, v_pages: Optional[torch.Tensor] = None):
+        self._h = _vp()
+        self.heads, self.kv_heads, self.head_dim = heads, kv_heads, head_dim
+        self.page_size, self.num_pages, self.dtype, self.kv_bits = page_size, num_pages, dtype, kv_bits
+        code = {torch.float16: SEGKV_F16, torch.bfloat16: SEGKV_BF16}.get(dtype, -1)
+        if page_bytes(kv_heads, head_dim, page_size, num_pages, kv_bits) == 0 or code < 0 or heads <= 0 or heads % kv_heads:
+            _check(-1, "segkv_pages_create")
+        if (k_pages is None) != (v_pages is None):
+            raise ValueError("k_pages and v_pages come together")
+        shape = (num_pages, kv_heads, page_size, head_dim) if kv_bits == 16 else (num_pages, kv_heads, page_size * (head_dim // 2 + 16))
+        kind = dtype if kv_bits == 16 else torch.uint8
+        if k_pages is None:
+            k_pages, v_pages = (torch.zeros(shape, dtype=kind, device="cuda") for _ in range(2))
+        for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+            if not t.is_cuda or not t.is_contiguous() or t.dtype != kind or tuple(t.shape) != shape:
+                raise ValueError(f"{name}: expected a contiguous CUDA tensor {shape} {kind}, got {tuple(t.shape)} {t.dtype}")
+        if v_pages.device != k_pages.device:
+            raise ValueError("k_pages and v_pages are on different devices")
+        self.device = k_pages.device
+        self.k_pages, self.v_pages = k_pages, v_pages
+        with torch.cuda.device(self.device):
+            _check(lib().segkv_pages_create(ctypes.byref(self._h), heads, kv_heads, head_dim, page_size, num_pages, code, kv_bits,
+                                            k_pages.data_ptr(), v_pages.data_ptr()), "segkv_pages_create")
+
+    # ------------------------------------------------------------ life cycle
+    def destroy(self) -> None:
+        if getattr(self, "_h", None) is not None and self._h:
+            with torch.cuda.device(self.device):
+                _check(lib().segkv_pages_destroy(self._h), "segkv_pages_destroy")
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.destroy()
+
+    # ------------------------------------------------------------- arguments
+    def _here(self, t: torch.Tensor, name: str) -> None:
+        if t.device != self.device:
+            raise ValueError(f"{name} is on {t.device}, the pages are on {self.device}")
+
+    def _index(self, table, lens, new_lens):
+        n = lens.shape[0] if lens.dim() == 1 else -1
+        for t, name in ((table, "table"), (lens, "lens"), (new_lens, "new_lens")):
+            if t is None:
+                continue
+            self._here(t, name)
+            if t.dtype != torch.int32 or not t.is_contiguous() or t.dim() != (2 if name == "table" else 1) or t.shape[0] != n:
+                raise ValueError(f"{name}: expected a contiguous int32 {'[n, entries]' if name == 'table' else '[n]'}, one row for each of "
+                                 f"lens' sequences, got {tuple(t.shape)} {t.dtype}")
+        return n, table.shape[1]
+
+    def _rows(self, t: torch.Tensor, n: int, heads: int, name: str):
+        """Pointer and row stride of [n, tokens, heads, head_dim] rows, each row contiguous, evenly spaced."""
+        self._here(t, name)
+        if t.dtype != self.dtype or t.dim() != 4 or t.shape[0] != n or t.shape[2] != heads or t.shape[3] != self.head_dim:
+            raise ValueError(f"{name}: expected [{n}, tokens, {heads}, {self.head_dim}] {self.dtype}, got {tuple(t.shape)} {t.dtype}")
+        T, st = t.shape[1], t.stride()
+        if t.numel() == 0:
+            return t.data_ptr(), heads * self.head_dim
+        if st[3] != 1 or (heads > 1 and st[2] != self.head_dim):
+            raise ValueError(f"{name}: a token's heads must be contiguous")
+        row = st[1] if T > 1 else st[0] if n > 1 else heads * self.head_dim
+        if n > 1 and st[0] != row * T:
+            raise ValueError(f"{name}: the tokens of the batch must be evenly spaced")
+        if row < heads * self.head_dim or row % 8:
+            raise ValueError(f"{name}: rows {row} elements apart: a multiple of 8 and no overlap is wanted")
+        return t.data_ptr(), row
+
+    def _dense(self, t: Optional[torch.Tensor], shape, name: str) -> Optional[int]:
+        if t is None:
+            return None
+        self._here(t, name)
+        if not t.is_contiguous() or t.dtype != self.dtype or tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name}: expected a contiguous tensor {tuple(shape)} {self.dtype}, got {tuple(t.shape)} {t.dtype}")
+        return t.data_ptr()
+
+    def _stream(self, stream) -> int:
+        if torch.cuda.current_device() != self.device.index:
+            raise ValueError(f"the pages are on {self.device}, the current device is cuda:{torch.cuda.current_device()}")
+        return _stream_ptr(stream)
+
+    # -------------------------------------------------------------- hot path
+    def append(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, new_lens: Optional[torch.Tensor] = None,
+               q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, rope_cos: Optional[torch.Tensor] = None,
+               rope_sin: Optional[torch.Tensor] = None, style="half", stream=None) -> Optional[torch.Tensor]:
+        """segkv_pages_append.  k, v [n, tokens, kv_heads, head_dim], q [n, tokens, heads, head_dim] (slices of a packed projection
+        will do); returns q_out, made here if it is not given."""
+        n, entries = self._index(table, lens, new_lens)
+        tokens = k.shape[1] if k.dim() == 4 else -1
+        if v.dim() != 4 or v.shape[1] != tokens or (q is not None and (q.dim() != 4 or q.shape[1] != tokens)):
+            raise ValueError("k, v and q need the same [n, tokens]")
+        kp, ks = self._rows(k, n, self.kv_heads, "k")
+        vp, vs = self._rows(v, n, self.kv_heads, "v")
+        qp, qs, qo, cos, sin, positions, code = None, 0, None, None, None, 0, 0
+        if q is not None:
+            qp, qs = self._rows(q, n, self.heads, "q")
+            shape = (n, tokens, self.heads, self.head_dim)
+            if q_out is None:
+                q_out = torch.empty(shape, dtype=self.dtype, device=self.device)
+            qo = self._dense(q_out, shape, "q_out")
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        if (rope_cos is None) != (rope_sin is None):
+            raise ValueError("rope_cos and rope_sin come together")
+        if rope_cos is not None:
+            for t, name in ((rope_cos, "rope_cos"), (rope_sin, "rope_sin")):
+                self._here(t, name)
+                if t.dtype != torch.float32 or not t.is_contiguous() or t.dim() != 2 or t.shape[1] != self.head_dim // 2 or t.shape[0] != rope_cos.shape[0]:
+                    raise ValueError(f"{name}: expected a contiguous float32 [positions, {self.head_dim // 2}], got {tuple(t.shape)} {t.dtype}")
+            cos, sin, positions = rope_cos.data_ptr(), rope_sin.data_ptr(), rope_cos.shape[0]
+            code = self.ROPE_STYLES[style] if isinstance(style, str) else int(style)
+        rc = lib().segkv_pages_append(self._h, n, tokens, kp, ks, vp, vs, table.data_ptr(), entries, lens.data_ptr(),
+                                      None if new_lens is None else new_lens.data_ptr(), qp, qs, qo, cos, sin, positions, code, self._stream(stream))
+        if rc:
+            _check(rc, "segkv_pages_append")
+        return q_out
+
+    def sdpa(self, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, out: Optional[torch.Tensor] = None,
+             alibi_slopes: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """segkv_pages_sdpa.  q, out [n, q_len, heads, head_dim]: the newest q_len tokens of every sequence."""
+        n, entries = self._index(table, lens, None)
+        qp, qs = self._rows(q, n, self.heads, "q")
+        if out is None:
+            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        op = self._dense(out, q.shape, "out")
+        sp = None
+        if alibi_slopes is not None:
+            self._here(alibi_slopes, "alibi_slopes")
+            if alibi_slopes.dtype != torch.float32 or tuple(alibi_slopes.shape) != (self.heads,) or not alibi_slopes.is_contiguous():
+                raise ValueError(f"alibi_slopes: expected a contiguous float32 [{self.heads}]")
+            sp = alibi_slopes.data_ptr()
+        rc = lib().segkv_pages_sdpa(self._h, n, q.shape[1], qp, qs, op, table.data_ptr(), entries, lens.data_ptr(), sp, self._stream(stream))
+        if rc:
+            _check(rc, "segkv_pages_sdpa")
+        return out
+
+    def read(self, table: torch.Tensor, lens: torch.Tensor, tokens: int, new_lens: Optional[torch.Tensor] = None,
+             k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None, stream=None):
+        """segkv_pages_read: (k, v) [n, tokens, kv_heads, head_dim], made here (zeros) if they are not given."""
+        n, entries = self._index(table, lens, new_lens)
+        shape = (n, tokens, self.kv_heads, self.head_dim)
+        k = torch.zeros(shape, dtype=self.dtype, device=self.device) if k is None else k
+        v = torch.zeros(shape, dtype=self.dtype, device=self.device) if v is None else v
+        kp, vp = self._dense(k, shape, "k"), self._dense(v, shape, "v")
+        rc = lib().segkv_pages_read(self._h, n, tokens, kp, vp, table.data_ptr(), entries, lens.data_ptr(),
+                                    None if new_lens is None else new_lens.data_ptr(), self._stream(stream))
+        if rc:
+            _check(rc, "segkv_pages_read")
+        return k, v
+
+    # ------------------------------------------------------------------ aids
+    def set_overlap(self, enable: bool) -> None:
+        _check(lib().segkv_pages_set_overlap(self._h, int(enable)), "segkv_pages_set_overlap")
+
+    def get_error(self) -> int:
+        flags = _int(0)
+        _check(lib().segkv_pages_get_error(self._h, ctypes.byref(flags)), "segkv_pages_get_error")
+        return flags.value
+
+    @property
+    def launch_count(self) -> int:
+        return int(lib().segkv_pages_launch_count(self._h))

@@ -25,11 +25,11 @@ LIB_PATH = os.path.join(_PKG, "libsegkv.so")
 
 SEGKV_F16, SEGKV_BF16 = 0, 1
 SEGKV_OK, SEGKV_EINVAL, SEGKV_ESTATE, SEGKV_ECAPACITY, SEGKV_ENOMEM, SEGKV_ECUDA, SEGKV_EDEVICE = 0, -1, -2, -3, -4, -5, -6
-SEGKV_DEV_BAD_PARENT, SEGKV_DEV_WAIT_LIMIT = 1, 2
+SEGKV_DEV_BAD_PARENT, SEGKV_DEV_WAIT_LIMIT, SEGKV_DEV_BAD_PAGE, SEGKV_DEV_BAD_POSITION = 1, 2, 4, 8
 
-_vp, _int, _i32p = ctypes.c_void_p, ctypes.c_int, ctypes.POINTER(ctypes.c_int32)
+_vp, _int, _i64, _i32p = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.POINTER(ctypes.c_int32)
 
-# name -> (restype, argtypes); one entry per symbol include/segkv.h declares
+# name -> (restype, argtypes); one entry per symbol include/segkv.h and include/segkv_pages.h declare
 SIGNATURES = {
     "segkv_create": (_int, [ctypes.POINTER(_vp)] + [_int] * 8),
     "segkv_create_growing": (_int, [ctypes.POINTER(_vp)] + [_int] * 9),
@@ -69,6 +69,15 @@ SIGNATURES = {
     "segkv_read_bandwidth": (_int, [_vp, ctypes.c_size_t, _int, ctypes.POINTER(ctypes.c_float), _vp]),
     "segkv_launch_count": (ctypes.c_longlong, [_vp]),
     "segkv_storage_bytes": (ctypes.c_size_t, [_int] * 7),
+    "segkv_pages_bytes": (ctypes.c_size_t, [_int] * 5),
+    "segkv_pages_create": (_int, [ctypes.POINTER(_vp)] + [_int] * 7 + [_vp, _vp]),
+    "segkv_pages_destroy": (_int, [_vp]),
+    "segkv_pages_append": (_int, [_vp, _int, _int, _vp, _i64, _vp, _i64, _vp, _int, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _int, _int, _vp]),
+    "segkv_pages_sdpa": (_int, [_vp, _int, _int, _vp, _i64, _vp, _vp, _int, _vp, _vp, _vp]),
+    "segkv_pages_read": (_int, [_vp, _int, _int, _vp, _vp, _vp, _int, _vp, _vp, _vp]),
+    "segkv_pages_set_overlap": (_int, [_vp, _int]),
+    "segkv_pages_get_error": (_int, [_vp, ctypes.POINTER(_int)]),
+    "segkv_pages_launch_count": (_i64, [_vp]),
     "segkv_strerror": (ctypes.c_char_p, [_int]),
     "segkv_last_cuda_error": (ctypes.c_char_p, []),
 }

@@ -1,0 +1,82 @@
+"""The paged cache's host checks, without a GPU."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import _pages as pg
+from paper_2401_05391_b200 import segkv as sk
+from paper_2401_05391_b200.pages import PagedKV, page_bytes
+
+
+def test_page_bytes():
+    assert page_bytes(8, 128, 16, 10) == 10 * 8 * 16 * 256
+    assert page_bytes(8, 128, 16, 10, 4) == 10 * 8 * 16 * 80
+    assert page_bytes(2, 64, 256, 1, 4) == 2 * 256 * 48 and page_bytes(1, 256, 32, 7, 4) == 7 * 32 * 144
+    for bad in ((0, 128, 16, 10, 16), (8, 96, 16, 10, 16), (8, 128, 24, 10, 16), (8, 128, 8, 10, 16), (8, 128, 512, 10, 16),
+                (8, 128, 16, 0, 16), (8, 128, 16, 10, 8), (8, 128, 256, 1 << 20, 16)):
+        assert page_bytes(*bad) == 0
+
+
+def test_create_and_null_handles_are_refused_without_a_gpu():
+    L, h = sk.lib(), ctypes.c_void_p()
+    mem = ctypes.create_string_buffer(4096 + 16)
+    at = (ctypes.addressof(mem) + 15) // 16 * 16
+    ok = [8, 2, 64, 16, 4, sk.SEGKV_F16, 16, at, at]
+    for i, v in ((0, 0), (0, 7), (1, 0), (2, 80), (3, 15), (4, -1), (5, 2), (6, 5), (7, None), (8, at + 8)):
+        a = list(ok)
+        a[i] = v
+        assert L.segkv_pages_create(ctypes.byref(h), *a) == sk.SEGKV_EINVAL and not h
+    assert L.segkv_pages_create(None, *ok) == sk.SEGKV_EINVAL
+    assert L.segkv_pages_destroy(None) == sk.SEGKV_OK
+    assert L.segkv_pages_append(None, 1, 1, at, 128, at, 128, at, 1, at, None, None, 0, None, None, None, 0, 0, None) == sk.SEGKV_EINVAL
+    assert L.segkv_pages_sdpa(None, 1, 1, at, 512, at, at, 1, at, None, None) == sk.SEGKV_EINVAL
+    assert L.segkv_pages_read(None, 1, 1, at, at, at, 1, at, None, None) == sk.SEGKV_EINVAL
+    assert L.segkv_pages_get_error(None, None) == sk.SEGKV_EINVAL and L.segkv_pages_set_overlap(None, 1) == sk.SEGKV_EINVAL
+    assert L.segkv_pages_launch_count(None) == sk.SEGKV_EINVAL
+
+
+def test_pages_have_to_be_on_a_gpu():
+    with pytest.raises(sk.SegKVError):
+        PagedKV(8, 3, 64, 16, 4)
+    with pytest.raises(ValueError):
+        PagedKV(8, 2, 64, 16, 4, k_pages=torch.zeros(4, 2, 16, 64, dtype=torch.float16), v_pages=torch.zeros(4, 2, 16, 64, dtype=torch.float16))
+    with pytest.raises(ValueError):
+        PagedKV(8, 2, 64, 16, 4, k_pages=torch.zeros(4, 2, 16, 64, dtype=torch.float16))
+
+
+def test_four_bit_rows_keep_half_a_step():
+    """The format itself: what the tests' plain form holds is within half a step of the value, and constant rows are held exactly."""
+    x = torch.randn(50, 64, generator=torch.Generator().manual_seed(1)).half()
+    x[0] = 3.25
+    c, s, z = pg.codes_of(x, torch.float16)
+    back = pg.values4(c[..., 0::2] | (c[..., 1::2] << 4), torch.cat([s, z], -1))
+    u = 2.0 ** -11
+    bound = s.double().repeat(1, 16) * (0.5 + 16 * u) + z.double().abs().repeat(1, 16) * 2 * u
+    assert ((back - x.double()).abs() <= bound).all() and torch.equal(back[0], x[0].double())
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_runs_of_blocks_cover_every_work_group_once(seed):
+    """The attention's schedule restated: CTA c takes blocks [total*c/G, total*(c+1)/G) of all work groups in order; the CTAs that
+    share a group are those that the kernel's closed form names, and no two groups that are shared begin in one CTA."""
+    rng = np.random.default_rng(seed)
+    G = int(rng.choice([1, 2, 7, 148, 296, 444]))
+    groups = [int(x) for x in rng.integers(1, rng.choice([2, 5, 60, 400]), size=int(rng.integers(1, 200)))]
+    total = sum(groups)
+    G = min(G, total)                                          # (as the kernel does)
+    cut = [total * c // G for c in range(G + 1)]
+    begins, base, seen = set(), 0, 0
+    for nb in groups:
+        real = [c for c in range(G) if max(cut[c], base) < min(cut[c + 1], base + nb)]
+        c0, c1 = ((base + 1) * G - 1) // total, ((base + nb) * G - 1) // total
+        if len(real) > 1:
+            assert real[0] == c0 and real[-1] == c1 and c0 not in begins
+            assert all(cut[c] < cut[c + 1] for c in range(c0, c1 + 1))      # no CTA in between is without a part
+            begins.add(c0)
+        else:
+            assert real == [c0] == [c1]
+        seen += nb
+        base += nb
+    assert seen == total
