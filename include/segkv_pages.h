@@ -29,8 +29,8 @@
  * s[0..3] and zero points z[0..3] of the row's four groups; channel d belongs to group d%4 and stands for
  * z + s*(code - 8).  (Interleaved groups, so that a tensor-core fragment made of a row's consecutive bytes
  * can be cut by group.)  A group's values x are held by
- *     step = (max x - min x)/15,  s = r(step),  z = r(min x + 8*step),  code = clamp(rint((x - z)/s) + 8, 0, 15)
- * (8 where s is 0; r rounds to the dtype, the rest is fp32), an error of about s/2.  A group with an Inf or NaN has s and
+ *     step = (max x - min x) * (1/15),  s = r(step),  z = r(min x + 8*step),  code = clamp(rint((x - z)/s) + 8, 0, 15)
+ * (8 where s is 0; r rounds to the dtype, the rest is fp32, 1/15 rounded to it), an error of about s/2.  A group with an Inf or NaN has s and
  * z NaN: all of it reads as NaN.
  */
 #ifndef SEGKV_PAGES_H

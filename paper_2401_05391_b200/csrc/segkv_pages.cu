@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kThreads) pages_append_kernel(const __grid_con
             float st[4], zt[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                st[j] = __fdiv_rn(__fsub_rn(mx[j], mn[j]), 15.f);
+                st[j] = __fmul_rn(__fsub_rn(mx[j], mn[j]), 0x1.111112p-4f);       // 1/15, rounded
                 zt[j] = __fadd_rn(mn[j], 8.f * st[j]);
             }
 #pragma unroll

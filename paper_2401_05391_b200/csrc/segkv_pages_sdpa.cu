@@ -42,33 +42,45 @@ struct Params {
 
 template <typename T> struct Num;
 template <> struct Num<__half> {
-    static constexpr uint32_t kMagic = 0x64006400u;          // 1024 in both halves: a code in the low bits adds itself
-    static constexpr float kMagicValue = 1024.f;
-    static constexpr uint32_t kMagicPlus8 = 0x64086408u;     // 1032
-    static constexpr float kLift = 6.f;                      // weights carry 2^kLift, so that small ones stay normal
-    static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t b) {
-        const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
-        return *reinterpret_cast<const uint32_t*>(&r);
-    }
-    static __device__ __forceinline__ void mma8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
-        asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(b0));
+    static constexpr float kLift = 6.f;                      // 16-bit rows: weights carry 2^kLift, so that small ones stay normal
+    static constexpr int kExpShift = 10, kExpBias = 15;
+    static __device__ __forceinline__ void mma8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
+        asm("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%7,%7,%7,%7};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(b0), "f"(0.f));
     }
 };
 template <> struct Num<__nv_bfloat16> {
-    static constexpr uint32_t kMagic = 0x43004300u;          // 128
-    static constexpr float kMagicValue = 128.f;
-    static constexpr uint32_t kMagicPlus8 = 0x43084308u;     // 136
     static constexpr float kLift = 0.f;
-    static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t b) {
-        const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
-        return *reinterpret_cast<const uint32_t*>(&r);
-    }
-    static __device__ __forceinline__ void mma8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
-        asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(b0));
+    static constexpr int kExpShift = 7, kExpBias = 127;
+    static __device__ __forceinline__ void mma8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
+        asm("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%7,%7,%7,%7};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(b0), "f"(0.f));
     }
 };
+
+// ---- 4-bit rows: codes as fp16, whatever the dtype ----------------------------------------------------------------------------
+// Two codes of a word, in bits 0-3 and 16-19, become fp16 numbers by or-ing them into 1024 (whose last place is 1); codes in bits 4-7 and
+// 20-23 count 16.  An fp16 product takes them exactly, so the queries (scaled by a power of two per column) and the weights are
+// fp16 for a bf16 cache too: 11 bits instead of 8, and half the shifts.
+constexpr uint32_t kMagic = 0x64006400u;
+constexpr float kLift4 = 6.f;
+__device__ __forceinline__ uint32_t codes_lo(uint32_t w) { return (w & 0x000F000Fu) | kMagic; }      // 1024 + c
+__device__ __forceinline__ uint32_t codes_hi(uint32_t w) { return (w & 0x00F000F0u) | kMagic; }      // 1024 + 16 c
+__device__ __forceinline__ uint32_t centred_lo(uint32_t w) {                                         // c - 8
+    const uint32_t x = codes_lo(w), k = 0x64086408u;                                                 // 1032
+    const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&k));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t centred_hi(uint32_t w) {                                         // (1024 + 16 c) / 16 - 72
+    const uint32_t x = codes_hi(w), m = 0x2C002C00u, k = 0xD480D480u;
+    const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&m), *reinterpret_cast<const __half2*>(&k));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ void mma_h(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1, float c2, float c3) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
 
 __device__ __forceinline__ uint32_t lds32(uint32_t a) {
     uint32_t r;
@@ -96,6 +108,9 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool real) {
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+// CTAs on an SM: what shared memory and registers allow.
+constexpr int ctas_per_sm(int D, int nc, int bits) { return bits == 16 ? (D == 256 ? 1 : 2) : (D == 256 || nc == 16 ? 2 : 3); }
+
 // Shared-memory shape of a variant.  NT: tiles of eight query columns; a warp's tile is SUB pieces of 16 keys.
 template <int D, int NT, int BITS> struct Shape {
     static constexpr int SUB = BITS == 16 ? (D == 64 ? 2 : 1) : (D == 256 ? 1 : 2);
@@ -108,7 +123,7 @@ template <int D, int NT, int BITS> struct Shape {
     static constexpr int MERGE = kWarps * 8 * 68 * 4;                         // 64 channels of eight columns of every warp
     static constexpr int ML = kWarps * NC * 2 * 4;
     static constexpr int SMEM = RING + MERGE + ML + 64;
-    static constexpr int CTAS = BITS == 16 ? (D == 256 ? 1 : 2) : (D == 256 ? 2 : 3);
+    static constexpr int CTAS = ctas_per_sm(D, NC, BITS);
     static constexpr int MT = D / 16;                                         // 16-channel tiles of the output
     static constexpr int SLOT = NC * (D + 2);
 };
@@ -123,6 +138,7 @@ template <int D> __device__ __forceinline__ uint32_t code_at(int k, int c) {
 
 struct Cursor {                      // a block of keys in the grid's order
     int v, h, b, nb, klen;
+    const int32_t* row;              // the sequence's pages
 };
 
 // Keys that column tile ct of sequence s reads, and how many blocks that makes (at least one: an empty sequence's output is written too).
@@ -143,12 +159,17 @@ __device__ __forceinline__ void extent(const Params& p, int v, int* klen, int* n
 }
 
 template <int NC, int KB>
+__device__ __forceinline__ void enter(const Params& p, Cursor& c) {
+    extent<NC, KB>(p, c.v, &c.klen, &c.nb, false);
+    c.row = p.table + (long long)(c.v / p.ctiles) * p.table_stride;
+}
+template <int NC, int KB>
 __device__ __forceinline__ void advance(const Params& p, Cursor& c, int V) {
     if (++c.b < c.nb) return;
     c.b = 0;
     if (++c.h < p.Hkv) return;
     c.h = 0;
-    if (++c.v < V) extent<NC, KB>(p, c.v, &c.klen, &c.nb, false);
+    if (++c.v < V) enter<NC, KB>(p, c);
 }
 
 template <typename T, int D, int NT, int BITS>
@@ -223,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
         ld.v = s_misc[0];
         ld.h = s_misc[1];
         ld.b = s_misc[2];
-        extent<NC, KB>(p, ld.v, &ld.klen, &ld.nb, false);
+        enter<NC, KB>(p, ld);
     }
     Cursor cur = ld;
     const int blocks = (int)(x1 - x0);
@@ -235,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
         for (int u = 0; u < SUB; ++u) {
             const int key = c.b * KB + warp * TK + 16 * u;
             pid[u] = 0;
-            if (key < c.klen) pid[u] = __ldg(p.table + (long long)(c.v / p.ctiles) * p.table_stride + (key >> p.page_log));
+            if (key < c.klen) pid[u] = __ldg(c.row + (key >> p.page_log));
         }
     };
     auto copy_tile = [&](const Cursor& c, int stage) {
@@ -304,16 +325,17 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
     const int kap = (g >> 1) + 4 * (g & 1);
     const int key_lo = BITS == 16 ? g : kap;
 
-    const float scale2 = kLog2e / sqrtf((float)D);
+    constexpr float kScale2 = D == 64 ? kLog2e * 0.125f : D == 128 ? kLog2e * 0.08838834764831845f : kLog2e * 0.0625f;
+    constexpr float kUp = BITS == 4 ? kLift4 : N::kLift;      // weights are 2^kUp times what they are
     uint32_t qf[NT][QJ][2];
-    float cinit[BITS == 4 ? NT : 1][4][2];                    // 4 bits: what the magic number adds to a group's sum
+    float cinit[BITS == 4 ? NT : 1][4][2];                    // 4 bits: what the magic number adds to a group's sum, negated
     uint32_t qsum[BITS == 4 ? NT : 1];                        // 4 bits: the groups' sums of q, in two parts (B operand)
-    int lim[NT][2];
-    float slope2[NT][2];
-    float mref[NT][2], lsum[NT][2];
+    int lim[NT][2];                                           // keys below it are seen
+    float scale2[NT][2], slope[NT][2];                        // of a raw score; of a key's distance, in raw scores
+    float mref[NT][2], thr[NT][2], base[NT][2], lsum[NT][2];  // reference, what moves it, its exponent; sum of weights
     float o[NT][MT][4];
     float zo[BITS == 4 ? NT : 1][4];
-    int vexp = -1;                                            // 4 bits, fp16: exponent that the values' scales are taken relative to
+    int vexp;                                                 // 4 bits: exponent that the values' scales are taken relative to
 
     unsigned long long x = x0;
     for (int done = 0; done < blocks;) {
@@ -330,6 +352,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
             const bool real = col < p.cols;
             const int row = real ? col / p.group : 0, hq = cur.h * p.group + (real ? col - row * p.group : 0);
             const char* qr = p.q + ((long long)s * p.q_len + row) * p.q_stride + (size_t)hq * (2 * D);
+            float unit = 1.f;                                 // of the column's scores
             if (BITS == 16) {
 #pragma unroll
                 for (int j = 0; j < QJ; ++j) {
@@ -337,31 +360,51 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                     qf[nt][j][1] = real ? __ldg(reinterpret_cast<const uint32_t*>(qr + (16 * j + 8 + 2 * t) * 2)) : 0u;
                 }
             } else {
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                uint4 raw[W];
+                float big = 0.f;
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
                     const int d = D == 256 ? (w < 4 ? 32 * t + 8 * w : 128 + 32 * t + 8 * (w - 4)) : (8 * W * t + 8 * w);
-                    uint4 r = make_uint4(0u, 0u, 0u, 0u);
-                    if (real) r = __ldg(reinterpret_cast<const uint4*>(qr + d * 2));
-                    const uint32_t pr[4] = {__byte_perm(r.x, r.z, 0x5410), __byte_perm(r.x, r.z, 0x7632),
-                                            __byte_perm(r.y, r.w, 0x5410), __byte_perm(r.y, r.w, 0x7632)};
+                    raw[w] = make_uint4(0u, 0u, 0u, 0u);
+                    if (real) raw[w] = __ldg(reinterpret_cast<const uint4*>(qr + d * 2));
+                    const uint32_t r4[4] = {raw[w].x, raw[w].y, raw[w].z, raw[w].w};
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {             // group j: channels j and j + 4 of the eight
-                        qf[nt][j * (W / 2) + (w >> 1)][w & 1] = pr[j];
-                        const float2 f = M::unpack(pr[j]);
-                        sum[j] += f.x + f.y;
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 f = M::unpack(r4[i]);
+                        big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
+                    }
+                }
+                big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+                big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+                // the column by a power of two: its largest value between 1 and 2 (values 2^-24 of it lose bits; 0, Inf and NaN stay so)
+                const int ex = min(max(__float_as_int(big) >> 23, 1), 253);
+                const float down = big > 0.f ? __int_as_float((254 - ex) << 23) : 1.f;
+                unit = big > 0.f ? __int_as_float(ex << 23) : 1.f;
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    const uint4 r = raw[w];
+                    const float2 e01 = M::unpack(r.x), e23 = M::unpack(r.y), e45 = M::unpack(r.z), e67 = M::unpack(r.w);
+                    const float lo[4] = {e01.x * down, e01.y * down, e23.x * down, e23.y * down};
+                    const float hi[4] = {e45.x * down, e45.y * down, e67.x * down, e67.y * down};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {             // group j: channels j and j + 4 of the eight; odd groups' codes count 16
+                        const float by = j & 1 ? 0.0625f : 1.f;
+                        qf[nt][j * (W / 2) + (w >> 1)][w & 1] = Mma<__half>::pack(lo[j] * by, hi[j] * by);
+                        const float2 f = Mma<__half>::unpack(qf[nt][j * (W / 2) + (w >> 1)][w & 1]);
+                        sum[j] += f.x + f.y;                  // (of what the product sees, times 16 where it counts 16)
                     }
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 1);
                     sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 2);
+                    const float off = sum[j] * (j & 1 ? -(1024.f + 128.f) : -1032.f);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        cinit[nt][j][e] = -(N::kMagicValue + 8.f) * __shfl_sync(0xffffffffu, sum[j], (2 * t + e) * 4);
+                    for (int e = 0; e < 2; ++e) cinit[nt][j][e] = __shfl_sync(0xffffffffu, off, (2 * t + e) * 4);
+                    if (j & 1) sum[j] *= 16.f;
                 }
-                // (2^-7: sums of 64 values of fp16 stay finite)
-                const float a = (t & 1 ? sum[2] : sum[0]) * 0.0078125f, b = (t & 1 ? sum[3] : sum[1]) * 0.0078125f;
+                const float a = t & 1 ? sum[2] : sum[0], b = t & 1 ? sum[3] : sum[1];
                 const uint32_t hi = M::pack(a, b);
                 const float2 hf = M::unpack(hi);
                 qsum[nt] = t < 2 ? hi : M::pack(a - hf.x, b - hf.y);
@@ -372,9 +415,10 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                 const bool r2 = c2 < p.cols;
                 const int row2 = r2 ? c2 / p.group : first_row;
                 lim[nt][e] = pos0 + row2 + 1;
-                slope2[nt][e] = p.slopes && r2 ? __ldg(p.slopes + cur.h * p.group + (c2 - row2 * p.group)) * kLog2e : 0.f;
-                mref[nt][e] = -INFINITY;
-                lsum[nt][e] = 0.f;
+                scale2[nt][e] = BITS == 4 ? kScale2 * __shfl_sync(0xffffffffu, unit, (2 * t + e) * 4) : kScale2;
+                slope[nt][e] = p.slopes && r2 ? __ldg(p.slopes + cur.h * p.group + (c2 - row2 * p.group)) * kLog2e / scale2[nt][e] : 0.f;
+                mref[nt][e] = thr[nt][e] = -INFINITY;
+                base[nt][e] = lsum[nt][e] = 0.f;
             }
 #pragma unroll
             for (int m = 0; m < MT; ++m)
@@ -385,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                 for (int e = 0; e < 4; ++e) zo[nt][e] = 0.f;
         }
         const int free_to = pos0 + first_row + 1;             // keys below it are seen by every row of the tile
-        vexp = -1;
+        vexp = 0;
 
         for (int blk = 0; blk < count; ++blk) {
             const int key0 = (cur.b + blk) * KB + warp * TK;
@@ -412,17 +456,17 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                             for (int nt = 0; nt < NT; ++nt) M::run(c[u][nt], a, qf[nt][j][0], qf[nt][j][1]);
                         }
                     } else {
-                        const uint32_t base = src + u * 16 * RB;
+                        const uint32_t rows = src + u * 16 * RB;
                         uint32_t wl[W], wh[W];
                         if constexpr (D == 64) {
-                            const uint32_t at = base + code_at<D>(kap, t >> 1) + (t & 1) * 8;
+                            const uint32_t at = rows + code_at<D>(kap, t >> 1) + (t & 1) * 8;
                             const uint2 a = lds64(at), b = lds64(at + 8 * RB);
                             wl[0] = a.x; wl[1] = a.y;
                             wh[0] = b.x; wh[1] = b.y;
                         } else {
 #pragma unroll
                             for (int q4 = 0; q4 < W / 4; ++q4) {
-                                const uint32_t at = base + code_at<D>(kap, t + 4 * q4);
+                                const uint32_t at = rows + code_at<D>(kap, t + 4 * q4);
                                 const uint4 a = lds128(at), b = lds128(at + 8 * RB);
                                 wl[4 * q4] = a.x; wl[4 * q4 + 1] = a.y; wl[4 * q4 + 2] = a.z; wl[4 * q4 + 3] = a.w;
                                 wh[4 * q4] = b.x; wh[4 * q4 + 1] = b.y; wh[4 * q4 + 2] = b.z; wh[4 * q4 + 3] = b.w;
@@ -435,27 +479,25 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                         // zero points: sum over groups of z * (sum of q in the group)
                         const uint32_t za = lds32(sc + 8 + (t & 1) * 4), zb = lds32(sc + 128 + 8 + (t & 1) * 4);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            float z[4] = {0.f, 0.f, 0.f, 0.f};
-                            N::mma8(z, za, zb, qsum[nt]);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) c[u][nt][e] = 128.f * z[e];
-                        }
-                        // codes: magic + code from the low bits, group by group, the magic's share taken off by the start value
+                        for (int nt = 0; nt < NT; ++nt) N::mma8(c[u][nt], za, zb, qsum[nt]);
+                        // codes, group by group; the magic's share is taken off by the start value
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             float acc[NT][4];
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                acc[nt][0] = acc[nt][2] = cinit[nt][j][0];
-                                acc[nt][1] = acc[nt][3] = cinit[nt][j][1];
-                            }
-#pragma unroll
                             for (int w2 = 0; w2 < W / 2; ++w2) {
-                                const uint32_t a[4] = {((wl[2 * w2] >> (4 * j)) & 0x000F000Fu) | N::kMagic, ((wh[2 * w2] >> (4 * j)) & 0x000F000Fu) | N::kMagic,
-                                                       ((wl[2 * w2 + 1] >> (4 * j)) & 0x000F000Fu) | N::kMagic, ((wh[2 * w2 + 1] >> (4 * j)) & 0x000F000Fu) | N::kMagic};
+                                uint32_t a[4] = {wl[2 * w2], wh[2 * w2], wl[2 * w2 + 1], wh[2 * w2 + 1]};
 #pragma unroll
-                                for (int nt = 0; nt < NT; ++nt) M::run(acc[nt], a, qf[nt][j * (W / 2) + w2][0], qf[nt][j * (W / 2) + w2][1]);
+                                for (int i = 0; i < 4; ++i) {
+                                    if (j >= 2) a[i] >>= 8;
+                                    a[i] = j & 1 ? codes_hi(a[i]) : codes_lo(a[i]);
+                                }
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) {
+                                    const uint32_t* b = qf[nt][j * (W / 2) + w2];
+                                    if (w2 == 0) mma_h(acc[nt], a, b[0], b[1], cinit[nt][j][0], cinit[nt][j][1], cinit[nt][j][0], cinit[nt][j][1]);
+                                    else mma_h(acc[nt], a, b[0], b[1], acc[nt][0], acc[nt][1], acc[nt][2], acc[nt][3]);
+                                }
                             }
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
@@ -467,22 +509,32 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                         }
                     }
                 }
-                // ---- scale, bias, mask, reference ---------------------------------------------------------------------------------
-                const bool masked = key0 + TK > free_to;
+                // ---- bias, mask, reference (raw scores) ------------------------------------------------------------------------------
+                if (p.slopes) {
+#pragma unroll
+                    for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                c[u][nt][e] = fmaf(slope[nt][e & 1], (float)(key0 + 16 * u + key_lo + (e >= 2 ? 8 : 0) + 1 - lim[nt][e & 1]), c[u][nt][e]);
+                }
+                if (key0 + TK > free_to) {
+#pragma unroll
+                    for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (key0 + 16 * u + key_lo + (e >= 2 ? 8 : 0) >= lim[nt][e & 1]) c[u][nt][e] = -INFINITY;
+                }
                 bool grow = false;
 #pragma unroll
                 for (int u = 0; u < SUB; ++u)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float v = c[u][nt][e] * scale2;
-                            const int key = key0 + 16 * u + key_lo + (e >= 2 ? 8 : 0);
-                            if (p.slopes) v = fmaf(slope2[nt][e & 1], (float)(key + 1 - lim[nt][e & 1]), v);
-                            if (masked && key >= lim[nt][e & 1]) v = -INFINITY;
-                            c[u][nt][e] = v;
-                            grow |= v > mref[nt][e & 1] + kSlack;
-                        }
+                        for (int e = 0; e < 4; ++e) grow |= c[u][nt][e] > thr[nt][e & 1];
                 if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
@@ -494,8 +546,10 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                            const float al = mref[nt][e] == -INFINITY ? 0.f : exp2f(mref[nt][e] - mx);
+                            const float al = mref[nt][e] == -INFINITY ? 1.f : exp2f((mref[nt][e] - mx) * scale2[nt][e]);
                             mref[nt][e] = mx;
+                            thr[nt][e] = mx + kSlack / scale2[nt][e];
+                            base[nt][e] = mx == -INFINITY ? 0.f : mx * scale2[nt][e] - kUp;
                             lsum[nt][e] *= al;
 #pragma unroll
                             for (int m = 0; m < MT; ++m) {
@@ -513,18 +567,17 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const float base = mref[nt][e] == -INFINITY ? 0.f : mref[nt][e] - N::kLift;
 #pragma unroll
                         for (int u = 0; u < SUB; ++u) {
-                            c[u][nt][e] = exp2f(c[u][nt][e] - base);
-                            c[u][nt][e + 2] = exp2f(c[u][nt][e + 2] - base);
+                            c[u][nt][e] = exp2f(fmaf(c[u][nt][e], scale2[nt][e], -base[nt][e]));
+                            c[u][nt][e + 2] = exp2f(fmaf(c[u][nt][e + 2], scale2[nt][e], -base[nt][e]));
                             lsum[nt][e] += c[u][nt][e] + c[u][nt][e + 2];
                         }
                     }
+                if constexpr (BITS == 16) {
 #pragma unroll
-                for (int u = 0; u < SUB; ++u) {
-                    if (u > 0 && key0 + 16 * u >= cur.klen) break;                     // (nothing was copied there)
-                    if (BITS == 16) {
+                    for (int u = 0; u < SUB; ++u) {
+                        if (u > 0 && key0 + 16 * u >= cur.klen) break;                 // (nothing was copied there)
                         uint32_t pf[NT][2];
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
@@ -540,31 +593,41 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) M::run(o[nt][m], a, pf[nt][0], pf[nt][1]);
                         }
-                    } else {
-                        const uint32_t sc = src + Sh::SOFF + TK * 16 + u * 256;
-                        // the values' scales go into the weights, in fp32 before their one rounding; the codes stay exact.  fp16 weights
-                        // times a scale would leave the type's range at either end, so scales are taken relative to a power of two
-                        const uint2 sl = lds64(sc + kap * 16), sh = lds64(sc + kap * 16 + 128);
-                        float unit = 1.f;
-                        if (N::kLift > 0.f) {
-                            uint32_t big = __vmaxu2(__vmaxu2(sl.x & 0x7FFF7FFFu, sl.y & 0x7FFF7FFFu), __vmaxu2(sh.x & 0x7FFF7FFFu, sh.y & 0x7FFF7FFFu));
-                            big = max(big & 0xFFFFu, big >> 16) >> 10;
-                            const int top = (int)__reduce_max_sync(0xffffffffu, min(big, 30u));
-                            if (top > vexp) {
-                                if (vexp >= 0) {
-                                    const float down = __int_as_float((127 + vexp - top) << 23);
+                    }
+                } else {
+                    // The values' scales go into the weights, in fp32 before their one rounding; the codes stay exact.  A weight times a
+                    // scale would leave fp16 at either end, so scales are taken relative to a power of two that only grows.
+                    const uint32_t scales = src + Sh::SOFF + TK * 16;
+                    uint2 sl[SUB], sh[SUB];
+                    uint32_t big = 0;
 #pragma unroll
-                                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                                        for (int m = 0; m < MT; ++m)
-#pragma unroll
-                                            for (int e = 0; e < 4; ++e) o[nt][m][e] *= down;
-                                }
-                                vexp = top;
-                            }
-                            unit = __int_as_float((127 + 15 - vexp) << 23);
+                    for (int u = 0; u < SUB; ++u) {
+                        sl[u] = sh[u] = make_uint2(0u, 0u);
+                        if (u == 0 || key0 + 16 * u < cur.klen) {                      // (else nothing was copied there)
+                            sl[u] = lds64(scales + (u * 16 + kap) * 16);
+                            sh[u] = lds64(scales + (u * 16 + kap) * 16 + 128);
                         }
-                        const float2 sl0 = M::unpack(sl.x), sl1 = M::unpack(sl.y), sh0 = M::unpack(sh.x), sh1 = M::unpack(sh.y);
+                        big = __vmaxu2(big, __vmaxu2(__vmaxu2(sl[u].x, sl[u].y), __vmaxu2(sh[u].x, sh[u].y)));     // (scales are not negative)
+                    }
+                    {
+                        constexpr uint32_t top_exp = (0x7FFFu >> N::kExpShift) - 1;    // (NaN: as large as a number can be)
+                        const int top = (int)min(__reduce_max_sync(0xffffffffu, max(big & 0xFFFFu, big >> 16)) >> N::kExpShift, top_exp);
+                        if (top > vexp) {
+                            const float down = __int_as_float(max(127 + vexp - top, 0) << 23);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) o[nt][m][e] *= down;
+                            vexp = top;
+                        }
+                    }
+                    const float unit = __int_as_float((127 + N::kExpBias - vexp) << 23);
+#pragma unroll
+                    for (int u = 0; u < SUB; ++u) {
+                        if (u > 0 && key0 + 16 * u >= cur.klen) break;
+                        const float2 sl0 = M::unpack(sl[u].x), sl1 = M::unpack(sl[u].y), sh0 = M::unpack(sh[u].x), sh1 = M::unpack(sh[u].y);
                         const float fl[4] = {sl0.x * unit, sl0.y * unit, sl1.x * unit, sl1.y * unit};
                         const float fh[4] = {sh0.x * unit, sh0.y * unit, sh1.x * unit, sh1.y * unit};
                         uint32_t pf[NT][4][2];
@@ -572,14 +635,14 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
-                                pf[nt][j][0] = movmatrix_trans(M::pack(c[u][nt][0] * fl[j], c[u][nt][1] * fl[j]));
-                                pf[nt][j][1] = movmatrix_trans(M::pack(c[u][nt][2] * fh[j], c[u][nt][3] * fh[j]));
+                                pf[nt][j][0] = movmatrix_trans(Mma<__half>::pack(c[u][nt][0] * fl[j], c[u][nt][1] * fl[j]));
+                                pf[nt][j][1] = movmatrix_trans(Mma<__half>::pack(c[u][nt][2] * fh[j], c[u][nt][3] * fh[j]));
                             }
                         // zero points: rows 0-3 of one more product are the groups'
                         {
                             uint32_t a[4] = {0u, 0u, 0u, 0u};
                             if (g < 4) {
-                                const uint32_t zp = sc + 8 + 2 * g + t * 16;
+                                const uint32_t zp = scales + u * 256 + 8 + 2 * g + t * 16;
                                 a[0] = lds16(zp) | (lds16(zp + 64) << 16);
                                 a[2] = lds16(zp + 128) | (lds16(zp + 192) << 16);
                             }
@@ -589,32 +652,37 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                         }
                         constexpr int VW = D / 64;            // code words of a value row that a lane weighs: channels g*D/8 + 8w ..
                         uint32_t w4[4][VW];
-                        const uint32_t base = src + Sh::VOFF + u * 16 * RB;
+                        const uint32_t rows = src + Sh::VOFF + u * 16 * RB;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {         // keys t, t + 4, t + 8, t + 12
                             if constexpr (D == 64) {
-                                w4[i][0] = lds32(base + code_at<D>(t + 4 * (i & 1), g >> 2) + (g & 3) * 4 + (i >> 1) * 8 * RB);
+                                w4[i][0] = lds32(rows + code_at<D>(t + 4 * (i & 1), g >> 2) + (g & 3) * 4 + (i >> 1) * 8 * RB);
                             } else if constexpr (D == 128) {
-                                const uint2 r = lds64(base + code_at<D>(t + 4 * (i & 1), g >> 1) + (g & 1) * 8 + (i >> 1) * 8 * RB);
+                                const uint2 r = lds64(rows + code_at<D>(t + 4 * (i & 1), g >> 1) + (g & 1) * 8 + (i >> 1) * 8 * RB);
                                 w4[i][0] = r.x; w4[i][1] = r.y;
                             } else {
-                                const uint4 r = lds128(base + code_at<D>(t + 4 * (i & 1), g) + (i >> 1) * 8 * RB);
+                                const uint4 r = lds128(rows + code_at<D>(t + 4 * (i & 1), g) + (i >> 1) * 8 * RB);
                                 w4[i][0] = r.x; w4[i][1] = r.y; w4[i][2] = r.z; w4[i][3] = r.w;
                             }
                         }
 #pragma unroll
                         for (int w = 0; w < VW; ++w) {
                             // keys t and t + 4 (t + 8 and t + 12) side by side: channels 0-3, then 4-7, of the word's eight
-                            const uint32_t al = __byte_perm(w4[0][w], w4[1][w], 0x5410), ah = __byte_perm(w4[0][w], w4[1][w], 0x7632);
-                            const uint32_t bl = __byte_perm(w4[2][w], w4[3][w], 0x5410), bh = __byte_perm(w4[2][w], w4[3][w], 0x7632);
+                            uint32_t r[4] = {__byte_perm(w4[0][w], w4[1][w], 0x5410), __byte_perm(w4[0][w], w4[1][w], 0x7632),
+                                             __byte_perm(w4[2][w], w4[3][w], 0x5410), __byte_perm(w4[2][w], w4[3][w], 0x7632)};
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
-                                const uint32_t a[4] = {N::sub(((al >> (4 * j)) & 0x000F000Fu) | N::kMagic, N::kMagicPlus8),
-                                                       N::sub(((ah >> (4 * j)) & 0x000F000Fu) | N::kMagic, N::kMagicPlus8),
-                                                       N::sub(((bl >> (4 * j)) & 0x000F000Fu) | N::kMagic, N::kMagicPlus8),
-                                                       N::sub(((bh >> (4 * j)) & 0x000F000Fu) | N::kMagic, N::kMagicPlus8)};
+                                uint32_t a[4];
 #pragma unroll
-                                for (int nt = 0; nt < NT; ++nt) M::run(o[nt][w * 4 + j], a, pf[nt][j][0], pf[nt][j][1]);
+                                for (int i = 0; i < 4; ++i) {
+                                    if (j == 2) r[i] >>= 8;
+                                    a[i] = j & 1 ? centred_hi(r[i]) : centred_lo(r[i]);
+                                }
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) {
+                                    float (&d)[4] = o[nt][w * 4 + j];
+                                    mma_h(d, a, pf[nt][j][0], pf[nt][j][1], d[0], d[1], d[2], d[3]);
+                                }
                             }
                         }
                     }
@@ -638,7 +706,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
 
         // ---- the work group's end: warps meet ------------------------------------------------------------------------------------
         if (BITS == 4) {                                      // zero points' part onto every channel of its group; units undone
-            const float up = vexp >= 0 ? __int_as_float((127 + vexp - 15) << 23) : 1.f;
+            const float up = __int_as_float((127 + vexp - N::kExpBias) << 23);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 float zg[4][2];
@@ -649,7 +717,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[nt][m][e] = fmaf(o[nt][m][e], N::kLift > 0.f ? up : 1.f, zg[m & 3][e & 1]);
+                    for (int e = 0; e < 4; ++e) o[nt][m][e] = fmaf(o[nt][m][e], up, zg[m & 3][e & 1]);
             }
         }
 #pragma unroll
@@ -662,7 +730,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                 l += __shfl_xor_sync(0xffffffffu, l, 16);
                 if (g == 0) {
                     float* ml = s_ml + (warp * NC + nt * 8 + 2 * t + e) * 2;
-                    ml[0] = mref[nt][e];
+                    ml[0] = mref[nt][e] == -INFINITY ? -INFINITY : mref[nt][e] * scale2[nt][e];
                     ml[1] = l;
                 }
             }
@@ -682,7 +750,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                 for (int w = 0; w < kWarps; ++w) top[e] = fmaxf(top[e], s_ml[(w * NC + nt * 8 + 2 * t + e) * 2]);
             float f[2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) f[e] = mref[nt][e] == -INFINITY ? 1.f : exp2f(mref[nt][e] - top[e]);     // (no weight: zeros, or NaN)
+            for (int e = 0; e < 2; ++e) f[e] = mref[nt][e] == -INFINITY ? 1.f : exp2f(mref[nt][e] * scale2[nt][e] - top[e]);     // (no weight: zeros, or NaN)
             float mtop = -INFINITY, lall = 0.f;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) mtop = fmaxf(mtop, s_ml[(w * NC + nt * 8 + mcol) * 2]);
@@ -846,8 +914,6 @@ cudaError_t launch_variant(const Params& p, int grid, bool pdl, cudaStream_t st)
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-int ctas_per_sm(int D, int bits) { return bits == 16 ? (D == 256 ? 1 : 2) : (D == 256 ? 2 : 3); }
-
 // Columns of a tile: 8, or 16 where there are more; at head_dim 256 always 8 (16 would not fit the registers).
 int columns_of(int D, int cols) { return D == 256 || cols <= 8 ? 8 : 16; }
 
@@ -860,7 +926,7 @@ cudaError_t launch_typed(int D, int nc, const Params& p, int grid, bool pdl, cud
 
 }  // namespace
 
-int pages_sdpa_grid(const segkv_pages& h) { return h.sm_count * ctas_per_sm(h.head_dim, h.bits); }
+int pages_sdpa_grid(const segkv_pages& h) { return h.sm_count * ctas_per_sm(h.head_dim, 8, h.bits); }
 size_t pages_sdpa_slot_floats(const segkv_pages& h) { return (size_t)(h.head_dim == 256 ? 8 : 16) * (h.head_dim + 2); }
 
 cudaError_t launch_pages_sdpa(const segkv_pages& h, const PageSdpaArgs& a, cudaStream_t st) {
@@ -873,7 +939,7 @@ cudaError_t launch_pages_sdpa(const segkv_pages& h, const PageSdpaArgs& a, cudaS
     p.cols = a.q_len * h.group;
     const int nc = columns_of(h.head_dim, p.cols);
     p.ctiles = (p.cols + nc - 1) / nc;
-    const int grid = pages_sdpa_grid(h);
+    const int grid = h.sm_count * ctas_per_sm(h.head_dim, nc, h.bits);
     if (h.dtype == SEGKV_BF16)
         return h.bits == 16 ? launch_typed<__nv_bfloat16, 16>(h.head_dim, nc, p, grid, a.pdl, st) : launch_typed<__nv_bfloat16, 4>(h.head_dim, nc, p, grid, a.pdl, st);
     return h.bits == 16 ? launch_typed<__half, 16>(h.head_dim, nc, p, grid, a.pdl, st) : launch_typed<__half, 4>(h.head_dim, nc, p, grid, a.pdl, st);

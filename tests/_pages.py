@@ -9,7 +9,7 @@ def codes_of(x, dtype):
     """(codes, scales, zero points) of rows x [..., D] of a 16-bit type, as the header gives them (fp32 steps)."""
     g = x.float().unflatten(-1, (-1, 4))
     lo, hi = g.amin(-2, keepdim=True), g.amax(-2, keepdim=True)
-    step = (hi - lo) / torch.full((), 15.0, device=x.device)          # (a Python number would be multiplied by its rounded inverse)
+    step = (hi - lo) * torch.full((), 1.0 / 15.0, device=x.device)
     s, z = step.to(dtype), (lo + 8.0 * step).to(dtype)
     bad = ~torch.isfinite(g).all(-2, keepdim=True) | ~torch.isfinite(s) | ~torch.isfinite(z)
     s, z = s.masked_fill(bad, math.nan), z.masked_fill(bad, math.nan)
