@@ -64,8 +64,14 @@ template <> struct Num<__nv_bfloat16> {
 // fp16 for a bf16 cache too: 11 bits instead of 8, and half the shifts.
 constexpr uint32_t kMagic = 0x64006400u;
 constexpr float kLift4 = 6.f;
-__device__ __forceinline__ uint32_t codes_lo(uint32_t w) { return (w & 0x000F000Fu) | kMagic; }      // 1024 + c
-__device__ __forceinline__ uint32_t codes_hi(uint32_t w) { return (w & 0x00F000F0u) | kMagic; }      // 1024 + 16 c
+// (w & mask) | magic in one instruction
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(kMagic));
+    return r;
+}
+__device__ __forceinline__ uint32_t codes_lo(uint32_t w) { return and_or(w, 0x000F000Fu); }          // 1024 + c
+__device__ __forceinline__ uint32_t codes_hi(uint32_t w) { return and_or(w, 0x00F000F0u); }          // 1024 + 16 c
 __device__ __forceinline__ uint32_t centred_lo(uint32_t w) {                                         // c - 8
     const uint32_t x = codes_lo(w), k = 0x64086408u;                                                 // 1032
     const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&k));
@@ -104,6 +110,9 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
 }
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool real) {     // zeros where it is not
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0));
+}
+__device__ __forceinline__ void cp16_all(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src));
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -259,8 +268,19 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
             if (key < c.klen) pid[u] = __ldg(c.row + (key >> p.page_log));
         }
     };
+    constexpr int CH = RB / 16;                               // 16-byte chunks of a row
+    constexpr int RI = 32 / CH;                               // rows that a warp's lanes copy at a time (4 bits, D 64: 16, D 256: 4)
+    const uint32_t ps = 1u << p.page_log;
+    const uint32_t head_bytes = ps * (uint32_t)(RB + (BITS == 4 ? 16 : 0));
+    const unsigned long long page_bytes = (unsigned long long)head_bytes * p.Hkv;
+    const long long v_behind = p.vp - p.kp;
+    const char* const k_lane = p.kp + lane * 16;              // this lane's chunk of a piece
+    const char* const s_lane = (lane < 16 ? p.kp : p.vp) + (size_t)ps * RB + (lane & 15) * 16;   // and of its scales: keys', then values'
+    const uint32_t c_lane = BITS == 16 ? 0 : code_at<D>(lane / CH, lane % CH);
+    const uint32_t cs_lane = Sh::SOFF + (lane < 16 ? 0 : TK * 16) + (lane & 15) * 16;
     auto copy_tile = [&](const Cursor& c, int stage) {
         const uint32_t dst = ring + stage * Sh::STAGE;
+        const uint32_t head_at = (uint32_t)c.h * head_bytes;
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
             const int key = c.b * KB + warp * TK + 16 * u;
@@ -270,34 +290,28 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                 if (lane == 0) atomicOr(p.err, SEGKV_DEV_BAD_PAGE);
                 page = 0;
             }
-            const int off = key & ((1 << p.page_log) - 1), left = c.klen - key;          // rows of the piece that exist
-            const size_t slab = ((size_t)page * p.Hkv + c.h) << p.page_log;              // row of the pool
+            const uint32_t off = (uint32_t)key & (ps - 1);
+            const int left = c.klen - key;                    // rows of the piece that exist
+            const unsigned long long at = (unsigned long long)(uint32_t)page * page_bytes + head_at;
+            const char* const k = k_lane + (at + off * RB);
             if (BITS == 16) {
-                constexpr int CH = RB / 16;                   // chunks of a row
-                const size_t at = (slab + off) * RB;
 #pragma unroll
-                for (int i = 0; i < 16 * CH / 32; ++i) {
-                    const int k = (i * 32 + lane) / CH, ch = (i * 32 + lane) % CH;
-                    const uint32_t to = dst + u * 16 * RB + k * RB + ((ch ^ (k & 7)) * 16);
-                    const size_t from = at + (size_t)(i * 32 + lane) * 16;
-                    cp16(to, p.kp + from, k < left);
-                    cp16(to + Sh::VOFF, p.vp + from, k < left);
+                for (int i = 0; i < 16 / RI; ++i) {
+                    const int r = i * RI + lane / CH, ch = lane % CH;
+                    const uint32_t to = dst + u * 16 * RB + r * RB + ((ch ^ (r & 7)) * 16);
+                    cp16(to, k + i * 512, r < left);
+                    cp16(to + Sh::VOFF, k + v_behind + i * 512, r < left);
                 }
             } else {
-                constexpr int CH = RB / 16;
-                const int ps = 1 << p.page_log;
-                const size_t blk = slab * (RB + 16), at = blk + (size_t)off * RB;
 #pragma unroll
-                for (int i = 0; i < (16 * CH + 31) / 32; ++i) {
-                    const int idx = i * 32 + lane;
-                    const uint32_t to = dst + u * 16 * RB + code_at<D>(idx / CH, idx % CH);
-                    cp16(to, p.kp + at + idx * 16, true);
-                    cp16(to + Sh::VOFF, p.vp + at + idx * 16, true);
+                for (int i = 0; i < 16 / RI; ++i) {
+                    // (the chunk's place RI rows further: 8 or 16 rows keep the pattern, 4 turn its bit 2)
+                    const uint32_t to = dst + u * 16 * RB + ((D == 256 && (i & 1) ? c_lane ^ 64u : c_lane) + i * RI * RB);
+                    cp16_all(to, k + i * 512);
+                    cp16_all(to + Sh::VOFF, k + v_behind + i * 512);
                 }
-                // scales: lanes 0-15 the keys', 16-31 the values'; rows that do not exist get zeros and stand for 0
-                const char* base = lane < 16 ? p.kp : p.vp;
-                cp16(dst + Sh::SOFF + (lane < 16 ? 0 : TK * 16) + (u * 16 + (lane & 15)) * 16,
-                     base + blk + (size_t)ps * RB + (off + (lane & 15)) * 16, (lane & 15) < left);
+                // rows that do not exist get scales of zero and stand for 0
+                cp16(dst + cs_lane + u * 256, s_lane + (at + off * 16), (lane & 15) < left);
             }
         }
         cp_commit();
@@ -643,8 +657,8 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                             uint32_t a[4] = {0u, 0u, 0u, 0u};
                             if (g < 4) {
                                 const uint32_t zp = scales + u * 256 + 8 + 2 * g + t * 16;
-                                a[0] = lds16(zp) | (lds16(zp + 64) << 16);
-                                a[2] = lds16(zp + 128) | (lds16(zp + 192) << 16);
+                                a[0] = __byte_perm(lds16(zp), lds16(zp + 64), 0x5410);
+                                a[2] = __byte_perm(lds16(zp + 128), lds16(zp + 192), 0x5410);
                             }
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt)
