@@ -32,8 +32,9 @@ struct Place {                   // where a token's rows lie
 };
 
 struct TokenParams {
-    int n, T, Hkv, page_log, num_pages, table_stride, rows;       // rows: of a token (key, value and query heads)
-    long long tokens;                                             // n * T
+    int n, T, Hkv, page_log, num_pages, table_stride;
+    int tokens, rows;                                             // n * T; rows of a token: key, value and query heads
+    int block_log, rows_cta;                                      // a CTA's tokens (a power of two) and how many of their rows it takes
     const int32_t *table, *lens, *new_lens;
     int* err;
 };
@@ -69,7 +70,7 @@ __device__ __forceinline__ Place place_of(const TokenParams& p, int s, int i, in
 }
 
 constexpr int kThreads = 256;
-constexpr int kTokenBlock = 16;  // neighbouring threads take the same head of this many tokens: their page rows lie side by side
+constexpr int kTokenBlock = 16;  // most tokens of a CTA
 
 struct AppendParams {
     TokenParams t;
@@ -80,76 +81,53 @@ struct AppendParams {
     int H, positions;
 };
 
-// Which token and which of its rows item `i` of the grid's order is; tokens in blocks, the block's tokens innermost.
-__device__ __forceinline__ bool item_of(const TokenParams& p, unsigned long long i, long long* token, int* row) {
-    const unsigned long long per = (unsigned long long)p.rows * kTokenBlock;
-    const long long full = p.tokens / kTokenBlock;
-    const unsigned long long blk = i / per;
-    unsigned rest = (unsigned)(i - blk * per);
-    if ((long long)blk > full) return false;
-    const unsigned width = (long long)blk < full ? kTokenBlock : (unsigned)(p.tokens - full * kTokenBlock);
-    if (width == 0) return false;
-    *row = (int)(rest / width);
-    *token = (long long)blk * kTokenBlock + (rest - (unsigned)*row * width);
-    return *row < p.rows;
+// A CTA's tokens: where they go, looked up once for all of their rows.
+__device__ __forceinline__ void find_places(const TokenParams& p, Place* s_place, int positions, bool reading) {
+    const int tok = (blockIdx.x << p.block_log) + threadIdx.x;
+    if (threadIdx.x < (1 << p.block_log)) {
+        Place r;
+        r.row = -1;
+        r.pos = 0;
+        if (tok < p.tokens) {
+            const int s = tok / p.T;
+            r = place_of(p, s, tok - s * p.T, positions, reading);
+        }
+        s_place[threadIdx.x] = r;
+    }
 }
 
-// One row of head_dim values by D/16 threads, each with eight values of the lower half and the eight that stand D/2 behind them,
-// so that a thread holds whole pairs of either rotary style and two whole code words.
-//
-// Rotation: products and sums rounded one by one (no contraction), so that the stored value is the one that the formula gives in
-// plain fp32 arithmetic: a code of the 4-bit form depends on its last bit.
-// 4 bits: the four interleaved groups' extremes go round the row's threads by shuffles (log2(D/16) steps of eight); a thread's
-// eight neighbouring channels are one 32-bit word of codes.
-// Bound: HBM for prompts (each value in once, each row out once), the chain length -> page -> store for a single token.
+// One thread's sixteen values of one row: rotated, and put where they belong.
 template <typename T, int D, int BITS, int STYLE>
-__global__ void __launch_bounds__(kThreads) pages_append_kernel(const __grid_constant__ AppendParams p) {
+__device__ __forceinline__ void store_row(const AppendParams& p, const Place& at, bool ok, int kind, int head, int token, int c,
+                                          uint4 lo, uint4 hi, const float* cs, const float* sn) {
     constexpr int TPR = D / 16;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const unsigned long long g = (unsigned long long)blockIdx.x * kThreads + threadIdx.x;
-    const int c = (int)(g % TPR);
-    long long token = 0;
-    int row = 0;
-    const bool there = item_of(p.t, g / TPR, &token, &row);
-    const int s = there ? (int)(token / p.t.T) : 0, i = there ? (int)(token - (long long)s * p.t.T) : 0;
-    const int kind = row < p.t.Hkv ? 0 : row < 2 * p.t.Hkv ? 1 : 2;                   // key, value, query
-    const int head = row - kind * p.t.Hkv;
-    uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
-    if (there) {
-        const char* src = kind == 0 ? p.k + token * p.k_stride : kind == 1 ? p.v + token * p.v_stride : p.q + token * p.q_stride;
-        src += (size_t)head * (D * 2) + c * 16;
-        lo = *reinterpret_cast<const uint4*>(src);
-        hi = *reinterpret_cast<const uint4*>(src + D);
-    }
-    Place at;
-    at.row = -1;
-    at.pos = 0;
-    if (there) at = place_of(p.t, s, i, STYLE ? p.positions : 0x7FFFFFFF, false);
-    const bool ok = at.row >= 0;
-    if (STYLE != 0 && ok && kind != 1) {
+    if (STYLE != 0 && kind != 1) {                            // (nothing real where !ok)
         uint32_t wl[4] = {lo.x, lo.y, lo.z, lo.w}, wh[4] = {hi.x, hi.y, hi.z, hi.w};
-        const float* cs = p.cos + (size_t)at.pos * (D / 2);
-        const float* sn = p.sin + (size_t)at.pos * (D / 2);
         if (STYLE == SEGKV_ROPE_HALF) {
+            float co[8], si[8];
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                *reinterpret_cast<float4*>(co + 4 * w) = *reinterpret_cast<const float4*>(cs + c * 8 + 4 * w);
+                *reinterpret_cast<float4*>(si + 4 * w) = *reinterpret_cast<const float4*>(sn + c * 8 + 4 * w);
+            }
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 const float2 a = Half<T>::up(wl[w]), b = Half<T>::up(wh[w]);
-                const float c0 = __ldg(cs + c * 8 + 2 * w), c1 = __ldg(cs + c * 8 + 2 * w + 1);
-                const float s0 = __ldg(sn + c * 8 + 2 * w), s1 = __ldg(sn + c * 8 + 2 * w + 1);
+                const float c0 = co[2 * w], c1 = co[2 * w + 1], s0 = si[2 * w], s1 = si[2 * w + 1];
                 wl[w] = Half<T>::down(__fsub_rn(__fmul_rn(a.x, c0), __fmul_rn(b.x, s0)), __fsub_rn(__fmul_rn(a.y, c1), __fmul_rn(b.y, s1)));
                 wh[w] = Half<T>::down(__fadd_rn(__fmul_rn(b.x, c0), __fmul_rn(a.x, s0)), __fadd_rn(__fmul_rn(b.y, c1), __fmul_rn(a.y, s1)));
             }
         } else {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
+            for (int u = 0; u < 2; ++u) {
+                float co[4], si[4];
+                *reinterpret_cast<float4*>(co) = *reinterpret_cast<const float4*>(cs + c * 4 + u * (D / 4));
+                *reinterpret_cast<float4*>(si) = *reinterpret_cast<const float4*>(sn + c * 4 + u * (D / 4));
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int pair = c * 4 + w + u * (D / 4);
-                    const float c0 = __ldg(cs + pair), s0 = __ldg(sn + pair);
+                for (int w = 0; w < 4; ++w) {
                     const float2 x = Half<T>::up(u ? wh[w] : wl[w]);
-                    const uint32_t y = Half<T>::down(__fsub_rn(__fmul_rn(x.x, c0), __fmul_rn(x.y, s0)),
-                                                     __fadd_rn(__fmul_rn(x.y, c0), __fmul_rn(x.x, s0)));
+                    const uint32_t y = Half<T>::down(__fsub_rn(__fmul_rn(x.x, co[w]), __fmul_rn(x.y, si[w])),
+                                                     __fadd_rn(__fmul_rn(x.y, co[w]), __fmul_rn(x.x, si[w])));
                     if (u) wh[w] = y; else wl[w] = y;
                 }
             }
@@ -171,6 +149,7 @@ __global__ void __launch_bounds__(kThreads) pages_append_kernel(const __grid_con
         }
     }
     if (BITS == 4) {                                          // (every thread: the row's threads exchange)
+        if (!__any_sync(0xffffffffu, ok && kind != 2)) return;
         float x[16];
         const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
         uint32_t bad = 0;
@@ -225,14 +204,19 @@ __global__ void __launch_bounds__(kThreads) pages_append_kernel(const __grid_con
                 z[2 * j] = b.x; z[2 * j + 1] = b.y;
             }
         }
+        const float inv[4] = {1.f / s[0], 1.f / s[1], 1.f / s[2], 1.f / s[3]};
         uint32_t code[2] = {0u, 0u};
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int j = e & 3;
             int cd = 8;
-            if (s[j] > 0.f && !(bad >> j & 1u)) {             // (far outside the range, where z's rounding is all there is, the
-                const float r = __fdiv_rn(__fsub_rn(x[e], z[j]), s[j]);       //  quotient may be large: clamped before it is an integer)
-                cd = __float2int_rn(fminf(fmaxf(rintf(r) + 8.f, 0.f), 15.f));
+            if (s[j] > 0.f && !(bad >> j & 1u)) {
+                // the quotient by a reciprocal, good to 2^-21 of it; where it stands that near a tie, by a division.  (Far outside the
+                // range, where z's rounding is all there is, it may be large: clamped before it is an integer.)
+                const float y = __fsub_rn(x[e], z[j]);
+                float r = y * inv[j], w1 = rintf(r);
+                if (fabsf(fabsf(r - w1) - 0.5f) < 1e-4f) w1 = rintf(__fdiv_rn(y, s[j]));
+                cd = __float2int_rn(fminf(fmaxf(w1 + 8.f, 0.f), 15.f));
             }
             code[e >> 3] |= (uint32_t)cd << (4 * (e & 7));
         }
@@ -247,54 +231,144 @@ __global__ void __launch_bounds__(kThreads) pages_append_kernel(const __grid_con
     }
 }
 
+// One row of head_dim values by D/16 threads, each with eight values of the lower half and the eight that stand D/2 behind them,
+// so that a thread holds whole pairs of either rotary style and two whole code words.
+//
+// Rotation: products and sums rounded one by one (no contraction), so that the stored value is the one that the formula gives in
+// plain fp32 arithmetic: a code of the 4-bit form depends on its last bit.
+// 4 bits: the four interleaved groups' extremes go round the row's threads by shuffles (log2(D/16) steps of eight); a thread's
+// eight neighbouring channels are one 32-bit word of codes.
+// A CTA takes up to 16 tokens and some or all of their rows, neighbouring thread groups the same head of neighbouring tokens, whose
+// page rows lie side by side; a token's page and its angles are fetched once, into shared memory.  Padding is not read.
+// Bound: HBM for prompts (each value in once, each row out once), the chain length -> page -> store for a single token.
+template <typename T, int D, int BITS, int STYLE>
+__global__ void __launch_bounds__(kThreads) pages_append_kernel(const __grid_constant__ AppendParams p) {
+    constexpr int TPR = D / 16, SLOTS = kThreads / TPR;
+    __shared__ Place s_place[kTokenBlock];
+    __shared__ __align__(16) float s_cos[STYLE ? kTokenBlock * (D / 2) : 4], s_sin[STYLE ? kTokenBlock * (D / 2) : 4];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    find_places(p.t, s_place, STYLE ? p.positions : 0x7FFFFFFF, false);
+    __syncthreads();
+    if (STYLE) {
+        for (int i = threadIdx.x; i < (D / 2) << p.t.block_log; i += kThreads) {
+            const Place a = s_place[i / (D / 2)];
+            if (a.row >= 0) {
+                s_cos[i] = __ldg(p.cos + (size_t)a.pos * (D / 2) + i % (D / 2));
+                s_sin[i] = __ldg(p.sin + (size_t)a.pos * (D / 2) + i % (D / 2));
+            }
+        }
+        __syncthreads();
+    }
+    const int c = threadIdx.x % TPR, slot = threadIdx.x / TPR;
+    const int row0 = blockIdx.y * p.t.rows_cta, rows = min(p.t.rows_cta, p.t.rows - row0);
+    const int items = rows << p.t.block_log;
+    const int tok0 = blockIdx.x << p.t.block_log;
+    constexpr int U = 2;                                      // rows of a thread in flight
+    for (int i0 = 0; i0 < items; i0 += U * SLOTS) {
+        uint4 lo_[U], hi_[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * SLOTS + slot, tl = i & ((1 << p.t.block_log) - 1), row = row0 + (i >> p.t.block_log);
+            lo_[u] = hi_[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (i < items && s_place[tl].row >= 0) {
+                const long long token = tok0 + tl;
+                const char* src = row < p.t.Hkv ? p.k + token * p.k_stride + (size_t)row * (D * 2)
+                                  : row < 2 * p.t.Hkv ? p.v + token * p.v_stride + (size_t)(row - p.t.Hkv) * (D * 2)
+                                                      : p.q + token * p.q_stride + (size_t)(row - 2 * p.t.Hkv) * (D * 2);
+                lo_[u] = *reinterpret_cast<const uint4*>(src + c * 16);
+                hi_[u] = *reinterpret_cast<const uint4*>(src + c * 16 + D);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i0 + u * SLOTS >= items) break;               // (every thread)
+            const int i = i0 + u * SLOTS + slot, tl = i & ((1 << p.t.block_log) - 1), row = row0 + (i >> p.t.block_log);
+            const Place at = s_place[tl];
+            const bool ok = i < items && at.row >= 0;
+            const int kind = row < p.t.Hkv ? 0 : row < 2 * p.t.Hkv ? 1 : 2;            // key, value, query
+            const int head = row - kind * p.t.Hkv;
+            store_row<T, D, BITS, STYLE>(p, at, ok, kind, head, tok0 + tl, c, lo_[u], hi_[u], s_cos + tl * (D / 2), s_sin + tl * (D / 2));
+        }
+    }
+}
+
 struct ReadParams {
     TokenParams t;
     const char *kp, *vp;
     char *k, *v;
 };
 
-// Eight neighbouring values of a row per thread.  Bound: HBM.
+// Eight neighbouring values of a row per thread, a CTA's tokens and rows as in the append.  Bound: HBM.
 template <typename T, int D, int BITS>
 __global__ void __launch_bounds__(kThreads) pages_read_kernel(const __grid_constant__ ReadParams p) {
-    constexpr int TPR = D / 8;
+    constexpr int TPR = D / 8, SLOTS = kThreads / TPR;
+    __shared__ Place s_place[kTokenBlock];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const unsigned long long g = (unsigned long long)blockIdx.x * kThreads + threadIdx.x;
-    const int c = (int)(g % TPR);
-    long long token;
-    int row;
-    if (!item_of(p.t, g / TPR, &token, &row)) return;
-    const int s = (int)(token / p.t.T), i = (int)(token - (long long)s * p.t.T);
-    const Place at = place_of(p.t, s, i, 0x7FFFFFFF, true);
-    if (at.row < 0) return;
-    const int kind = row < p.t.Hkv ? 0 : 1, head = row - kind * p.t.Hkv;
-    const long long first = at.row + ((long long)head << p.t.page_log);
-    const char* pages = kind == 0 ? p.kp : p.vp;
-    uint4 out;
-    if (BITS == 16) {
-        out = *reinterpret_cast<const uint4*>(pages + (size_t)first * (D * 2) + c * 16);
-    } else {
-        const int ps = 1 << p.t.page_log, in_page = (int)(first & (ps - 1));
-        const char* blk = pages + (size_t)(first >> p.t.page_log) * ((size_t)ps * (D / 2 + 16));
-        const uint32_t code = reinterpret_cast<const uint32_t*>(blk + (size_t)in_page * (D / 2))[c];
-        const uint4 sc = *reinterpret_cast<const uint4*>(blk + (size_t)ps * (D / 2) + in_page * 16);
-        const float2 s0 = Half<T>::up(sc.x), s1 = Half<T>::up(sc.y), z0 = Half<T>::up(sc.z), z1 = Half<T>::up(sc.w);
-        const float s4[4] = {s0.x, s0.y, s1.x, s1.y}, z4[4] = {z0.x, z0.y, z1.x, z1.y};
-        float x[8];
+    find_places(p.t, s_place, 0x7FFFFFFF, true);
+    __syncthreads();
+    const int c = threadIdx.x % TPR, slot = threadIdx.x / TPR;
+    const int row0 = blockIdx.y * p.t.rows_cta, rows = min(p.t.rows_cta, p.t.rows - row0);
+    const int items = rows << p.t.block_log;
+    const int tok0 = blockIdx.x << p.t.block_log;
+    const int ps = 1 << p.t.page_log;
+    constexpr int U = 4;                                      // rows of a thread in flight
+    for (int i0 = 0; i0 < items; i0 += U * SLOTS) {
+        uint4 x[U];
+        uint32_t code[U];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = fmaf((float)((int)(code >> (4 * e) & 15u) - 8), s4[e & 3], z4[e & 3]);
-        out = make_uint4(Half<T>::down(x[0], x[1]), Half<T>::down(x[2], x[3]), Half<T>::down(x[4], x[5]), Half<T>::down(x[6], x[7]));
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * SLOTS + slot, tl = i & ((1 << p.t.block_log) - 1), row = row0 + (i >> p.t.block_log);
+            x[u] = make_uint4(0u, 0u, 0u, 0u);
+            code[u] = 0u;
+            if (i >= items || s_place[tl].row < 0) continue;
+            const int kind = row < p.t.Hkv ? 0 : 1, head = row - kind * p.t.Hkv;
+            const long long first = s_place[tl].row + ((long long)head << p.t.page_log);
+            const char* pages = kind == 0 ? p.kp : p.vp;
+            if (BITS == 16) {
+                x[u] = *reinterpret_cast<const uint4*>(pages + (size_t)first * (D * 2) + c * 16);
+            } else {
+                const int in_page = (int)(first & (ps - 1));
+                const char* blk = pages + (size_t)(first >> p.t.page_log) * ((size_t)ps * (D / 2 + 16));
+                code[u] = reinterpret_cast<const uint32_t*>(blk + (size_t)in_page * (D / 2))[c];
+                x[u] = *reinterpret_cast<const uint4*>(blk + (size_t)ps * (D / 2) + in_page * 16);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * SLOTS + slot, tl = i & ((1 << p.t.block_log) - 1), row = row0 + (i >> p.t.block_log);
+            if (i >= items || s_place[tl].row < 0) continue;
+            const int kind = row < p.t.Hkv ? 0 : 1, head = row - kind * p.t.Hkv;
+            uint4 out = x[u];
+            if (BITS == 4) {
+                const float2 s0 = Half<T>::up(x[u].x), s1 = Half<T>::up(x[u].y), z0 = Half<T>::up(x[u].z), z1 = Half<T>::up(x[u].w);
+                const float s4[4] = {s0.x, s0.y, s1.x, s1.y}, z4[4] = {z0.x, z0.y, z1.x, z1.y};
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = fmaf((float)((int)(code[u] >> (4 * e) & 15u) - 8), s4[e & 3], z4[e & 3]);
+                out = make_uint4(Half<T>::down(v[0], v[1]), Half<T>::down(v[2], v[3]), Half<T>::down(v[4], v[5]), Half<T>::down(v[6], v[7]));
+            }
+            char* dst = (kind == 0 ? p.k : p.v) + ((size_t)(tok0 + tl) * p.t.Hkv + head) * (D * 2) + c * 16;
+            *reinterpret_cast<uint4*>(dst) = out;
+        }
     }
-    char* dst = (kind == 0 ? p.k : p.v) + ((size_t)token * p.t.Hkv + head) * (D * 2) + c * 16;
-    *reinterpret_cast<uint4*>(dst) = out;
 }
 
 template <typename P>
-cudaError_t launch(void (*kernel)(P), const P& p, unsigned long long threads, bool pdl, cudaStream_t st) {
-    const unsigned long long blocks = (threads + kThreads - 1) / kThreads;
-    if (blocks > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
+cudaError_t launch(void (*kernel)(P), P& p, int slots, int sm_count, bool pdl, cudaStream_t st) {
+    // tokens of a CTA: 16, fewer where there are fewer; rows of a CTA: all, or as many fewer as give the GPU four CTAs an SM, but
+    // one row for each of a CTA's thread groups at least
+    p.t.block_log = 0;
+    while ((1 << p.t.block_log) < kTokenBlock && (2 << p.t.block_log) <= p.t.tokens) p.t.block_log++;
+    const long long blocks = ((long long)p.t.tokens + (1 << p.t.block_log) - 1) >> p.t.block_log;
+    int rows = p.t.rows;
+    while (rows > 1 && (rows << p.t.block_log) > slots && blocks * ((p.t.rows + rows - 1) / rows) < 4LL * sm_count) rows = (rows + 1) / 2;
+    p.t.rows_cta = rows;
+    const int chunks = (p.t.rows + rows - 1) / rows;
+    if (chunks > 65535) return cudaErrorInvalidConfiguration;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)blocks, 1, 1);
+    cfg.gridDim = dim3((unsigned)blocks, (unsigned)chunks, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -310,7 +384,7 @@ cudaError_t launch(void (*kernel)(P), const P& p, unsigned long long threads, bo
 TokenParams token_params(const segkv_pages& h, const PageTokens& t, int rows) {
     TokenParams p;
     p.n = t.n; p.T = t.tokens; p.Hkv = h.kv_heads; p.page_log = h.page_log; p.num_pages = h.num_pages;
-    p.table_stride = t.table_stride; p.rows = rows; p.tokens = (long long)t.n * t.tokens;
+    p.table_stride = t.table_stride; p.rows = rows; p.tokens = t.n * t.tokens;
     p.table = t.table; p.lens = t.lens; p.new_lens = t.new_lens; p.err = h.err_word;
     return p;
 }
@@ -342,7 +416,7 @@ cudaError_t launch_pages_append(const segkv_pages& h, const PageAppendArgs& a, c
     p.kp = h.kp; p.vp = h.vp; p.q_out = (char*)a.q_out;
     p.cos = a.cos; p.sin = a.sin; p.H = h.heads; p.positions = a.positions;
     auto kernel = h.dtype == SEGKV_BF16 ? append_of<__nv_bfloat16>(h.head_dim, h.bits, a.style) : append_of<__half>(h.head_dim, h.bits, a.style);
-    return launch(kernel, p, (unsigned long long)p.t.tokens * p.t.rows * (h.head_dim / 16), a.t.pdl, st);
+    return launch(kernel, p, kThreads / (h.head_dim / 16), h.sm_count, a.t.pdl, st);
 }
 
 cudaError_t launch_pages_read(const segkv_pages& h, const PageTokens& t, void* k_out, void* v_out, cudaStream_t st) {
@@ -350,7 +424,7 @@ cudaError_t launch_pages_read(const segkv_pages& h, const PageTokens& t, void* k
     p.t = token_params(h, t, 2 * h.kv_heads);
     p.kp = h.kp; p.vp = h.vp; p.k = (char*)k_out; p.v = (char*)v_out;
     auto kernel = h.dtype == SEGKV_BF16 ? read_of<__nv_bfloat16>(h.head_dim, h.bits) : read_of<__half>(h.head_dim, h.bits);
-    return launch(kernel, p, (unsigned long long)p.t.tokens * p.t.rows * (h.head_dim / 8), t.pdl, st);
+    return launch(kernel, p, kThreads / (h.head_dim / 8), h.sm_count, t.pdl, st);
 }
 
 }  // namespace segkv_impl

@@ -28,7 +28,7 @@ int check_call(const segkv_pages* h, int n, int tokens, const int32_t* table, in
     if (dev != h->device) return SEGKV_EINVAL;
     if (n == 0 || tokens == 0) return SEGKV_OK;
     if (!table || !lens || table_stride <= 0 || !aligned(table, 4) || !aligned(lens, 4)) return SEGKV_EINVAL;
-    if ((long long)n * tokens > 0x7FFFFFFFLL) return SEGKV_EINVAL;
+    if ((long long)n * tokens > 0x7FFFFF00LL) return SEGKV_EINVAL;
     return SEGKV_OK;
 }
 

@@ -21,7 +21,7 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps, kStages = 3;
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr float kLog2e = 1.4426950408889634f;
 // A column's weights are taken relative to a reference that is only moved when a score exceeds it by 2^kSlack.
 constexpr float kSlack = 8.f;
@@ -118,7 +118,8 @@ __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_grou
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // CTAs on an SM: what shared memory and registers allow.
-constexpr int ctas_per_sm(int D, int nc, int bits) { return bits == 16 ? (D == 256 ? 1 : 2) : (D == 256 || nc == 16 ? 2 : 3); }
+constexpr int ctas_per_sm(int D, int nc, int bits) { return bits == 16 ? (D == 256 ? 1 : 2) : D == 256 || nc == 16 ? 2 : 3; }
+constexpr int kStages = 3;
 
 // Shared-memory shape of a variant.  NT: tiles of eight query columns; a warp's tile is SUB pieces of 16 keys.
 template <int D, int NT, int BITS> struct Shape {
@@ -448,7 +449,18 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
         for (int blk = 0; blk < count; ++blk) {
             const int key0 = (cur.b + blk) * KB + warp * TK;
             cp_wait<kStages - 2>();
-            __syncwarp();
+            __syncwarp();                                     // every lane's copies are seen, and every lane is done with that stage
+            // the next copy, into the stage of the tile before this one
+            if (copied < blocks) {
+                copy_tile(ld, fill);
+                ++copied;
+                if (copied < blocks) {
+                    advance<NC, KB>(p, ld, V);
+                    find_pages(ld);
+                }
+            } else {
+                cp_commit();
+            }
             if (key0 < cur.klen) {
                 const uint32_t src = ring + stage * Sh::STAGE;
                 float c[SUB][NT][4];
@@ -702,18 +714,6 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                     }
                 }
             }
-            __syncwarp();
-            // ---- the next copy, into the stage of the tile before this one ----------------------------------------------------------
-            if (copied < blocks) {
-                copy_tile(ld, fill);
-                ++copied;
-                if (copied < blocks) {
-                    advance<NC, KB>(p, ld, V);
-                    find_pages(ld);
-                }
-            } else {
-                cp_commit();
-            }
             stage = stage + 1 == kStages ? 0 : stage + 1;
             fill = fill + 1 == kStages ? 0 : fill + 1;
         }
@@ -813,83 +813,75 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
         }
         if (!whole) {
             // ---- partial results: the last CTA of the work group folds them -------------------------------------------------------
-            __threadfence();
             __syncthreads();
-            if (tid == 0) s_misc[3] = atomicAdd(p.tickets + c0, 1);
+            if (tid == 0) {
+                __threadfence();                              // (the CTA's writes, behind the barrier above)
+                s_misc[3] = atomicAdd(p.tickets + c0, 1);
+                __threadfence();
+            }
             __syncthreads();
             if (s_misc[3] == c1 - c0) {
-                __threadfence();
                 if (tid == 0) p.tickets[c0] = 0;              // as the next launch expects it
                 const int parts = c1 - c0 + 1;
-                auto part = [&](int i) { return p.ws + ((size_t)(c0 + i) * 2 + (i == 0 ? 1 : 0)) * Sh::SLOT; };
-                constexpr int PG = kThreads / NC;             // threads of a column
-                const int fcol = tid % NC, fp = tid / NC;
-                float* s_top = s_merge;                       // [PG][NC], then [NC]
-                float* s_sum = s_merge + kThreads;
-                float* s_f = s_merge + 2 * kThreads;          // [32][NC]
-                float mx = -INFINITY;
-                for (int i = fp; i < parts; i += PG) mx = fmaxf(mx, __ldcg(part(i) + NC * D + fcol));
-                s_top[tid] = mx;
-                __syncthreads();
-                mx = -INFINITY;
+                constexpr int AT = D == 256 ? 4 : 8;          // parts whose loads are in flight together
 #pragma unroll
-                for (int i = 0; i < PG; ++i) mx = fmaxf(mx, s_top[i * NC + fcol]);
-                float sum = 0.f;
-                for (int i = fp; i < parts; i += PG) {
-                    const float m = __ldcg(part(i) + NC * D + fcol), l = __ldcg(part(i) + NC * D + NC + fcol);
-                    sum += m == -INFINITY ? l : l * exp2f(m - mx);
-                }
-                s_sum[tid] = sum;
-                float4 acc[NT][D / 64];
+                for (int nt = 0; nt < NT; ++nt) {
+                    const int lcol = nt * 8 + mcol, col = ct * NC + lcol;
+                    float top = -INFINITY, sum = 0.f;
+                    float4 acc[D / 64];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                    for (int r = 0; r < D / 64; ++r) acc[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int i0 = 0; i0 < parts; i0 += AT) {
+                        float m[AT], l[AT];
+                        float4 v[AT][D / 64];
 #pragma unroll
-                    for (int r = 0; r < D / 64; ++r) acc[nt][r] = make_float4(0.f, 0.f, 0.f, 0.f);
-                for (int i0 = 0; i0 < parts; i0 += 32) {
-                    __syncthreads();
-                    for (int i = fp; i < 32 && i0 + i < parts; i += PG) {
-                        const float m = __ldcg(part(i0 + i) + NC * D + fcol);
-                        s_f[i * NC + fcol] = m == -INFINITY ? 1.f : exp2f(m - mx);     // (no weight: its values are zeros, or NaN)
-                    }
-                    __syncthreads();
-                    const int n = min(32, parts - i0);
-#pragma unroll 4
-                    for (int i = 0; i < n; ++i) {
-                        const float* src = part(i0 + i);
+                        for (int i = 0; i < AT; ++i) {
+                            m[i] = -INFINITY;
+                            l[i] = 0.f;
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            const float fi = s_f[i * NC + nt * 8 + mcol];
+                            for (int r = 0; r < D / 64; ++r) v[i][r] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (i0 + i >= parts) continue;
+                            const float* src = p.ws + ((size_t)(c0 + i0 + i) * 2 + (i0 + i == 0 ? 1 : 0)) * Sh::SLOT;
+                            m[i] = __ldcg(src + NC * D + lcol);
+                            l[i] = __ldcg(src + NC * D + NC + lcol);
+#pragma unroll
+                            for (int r = 0; r < D / 64; ++r) v[i][r] = __ldcg(reinterpret_cast<const float4*>(src + lcol * D + 64 * r + mloc));
+                        }
+                        float mx = top;
+#pragma unroll
+                        for (int i = 0; i < AT; ++i) mx = fmaxf(mx, m[i]);
+                        const float keep = top == -INFINITY ? 1.f : exp2f(top - mx);
+                        sum *= keep;
+#pragma unroll
+                        for (int r = 0; r < D / 64; ++r) {
+                            acc[r].x *= keep; acc[r].y *= keep; acc[r].z *= keep; acc[r].w *= keep;
+                        }
+                        top = mx;
+#pragma unroll
+                        for (int i = 0; i < AT; ++i) {
+                            const float fi = m[i] == -INFINITY ? 1.f : exp2f(m[i] - mx);        // (no weight: zeros, or NaN)
+                            sum = fmaf(l[i], fi, sum);
 #pragma unroll
                             for (int r = 0; r < D / 64; ++r) {
-                                const int d = 64 * r + mloc;
-                                const float4 b = __ldcg(reinterpret_cast<const float4*>(src + (nt * 8 + mcol) * D + d));
-                                acc[nt][r].x = fmaf(b.x, fi, acc[nt][r].x);
-                                acc[nt][r].y = fmaf(b.y, fi, acc[nt][r].y);
-                                acc[nt][r].z = fmaf(b.z, fi, acc[nt][r].z);
-                                acc[nt][r].w = fmaf(b.w, fi, acc[nt][r].w);
+                                acc[r].x = fmaf(v[i][r].x, fi, acc[r].x);
+                                acc[r].y = fmaf(v[i][r].y, fi, acc[r].y);
+                                acc[r].z = fmaf(v[i][r].z, fi, acc[r].z);
+                                acc[r].w = fmaf(v[i][r].w, fi, acc[r].w);
                             }
                         }
                     }
-                }
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const int col = ct * NC + nt * 8 + mcol;
-                    float l = 0.f;
-#pragma unroll
-                    for (int i = 0; i < PG; ++i) l += s_sum[i * NC + nt * 8 + mcol];
-                    const float inv = l == 0.f ? 0.f : 1.f / l;
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
                     if (col < p.cols) {
                         const int row = col / p.group, hq = cur.h * p.group + (col - row * p.group);
 #pragma unroll
                         for (int r = 0; r < D / 64; ++r) {
                             uint2 w2;
-                            w2.x = M::pack(acc[nt][r].x * inv, acc[nt][r].y * inv);
-                            w2.y = M::pack(acc[nt][r].z * inv, acc[nt][r].w * inv);
+                            w2.x = M::pack(acc[r].x * inv, acc[r].y * inv);
+                            w2.y = M::pack(acc[r].z * inv, acc[r].w * inv);
                             *reinterpret_cast<uint2*>(p.out + ((((size_t)s * p.q_len + row) * p.H + hq) * D + 64 * r + mloc) * 2) = w2;
                         }
                     }
                 }
-                __syncthreads();                              // s_merge is the next work group's
             }
         }
         done += count;
