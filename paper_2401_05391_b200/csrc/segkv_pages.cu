@@ -16,12 +16,28 @@ template <> struct Half<__half> {
         const __half2 t = __floats2half2_rn(a, b);
         return *reinterpret_cast<const uint32_t*>(&t);
     }
+    static __device__ __forceinline__ uint32_t least(uint32_t a, uint32_t b) {       // (NaN stays)
+        const __half2 t = __hmin2_nan(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+        return *reinterpret_cast<const uint32_t*>(&t);
+    }
+    static __device__ __forceinline__ uint32_t most(uint32_t a, uint32_t b) {
+        const __half2 t = __hmax2_nan(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+        return *reinterpret_cast<const uint32_t*>(&t);
+    }
 };
 template <> struct Half<__nv_bfloat16> {
     static constexpr uint32_t kInf = 0x7F80u, kNan = 0x7FFFu;
     static __device__ __forceinline__ float2 up(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
     static __device__ __forceinline__ uint32_t down(float a, float b) {
         const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&t);
+    }
+    static __device__ __forceinline__ uint32_t least(uint32_t a, uint32_t b) {
+        const __nv_bfloat162 t = __hmin2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+        return *reinterpret_cast<const uint32_t*>(&t);
+    }
+    static __device__ __forceinline__ uint32_t most(uint32_t a, uint32_t b) {
+        const __nv_bfloat162 t = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
         return *reinterpret_cast<const uint32_t*>(&t);
     }
 };
@@ -70,7 +86,7 @@ __device__ __forceinline__ Place place_of(const TokenParams& p, int s, int i, in
 }
 
 constexpr int kThreads = 256;
-constexpr int kTokenBlock = 16;  // most tokens of a CTA
+constexpr int kTokenBlock = 8;   // most tokens of a CTA
 
 struct AppendParams {
     TokenParams t;
@@ -96,199 +112,186 @@ __device__ __forceinline__ void find_places(const TokenParams& p, Place* s_place
     }
 }
 
-// One thread's sixteen values of one row: rotated, and put where they belong.
-template <typename T, int D, int BITS, int STYLE>
-__device__ __forceinline__ void store_row(const AppendParams& p, const Place& at, bool ok, int kind, int head, int token, int c,
-                                          uint4 lo, uint4 hi, const float* cs, const float* sn) {
-    constexpr int TPR = D / 16;
-    if (STYLE != 0 && kind != 1) {                            // (nothing real where !ok)
-        uint32_t wl[4] = {lo.x, lo.y, lo.z, lo.w}, wh[4] = {hi.x, hi.y, hi.z, hi.w};
-        if (STYLE == SEGKV_ROPE_HALF) {
-            float co[8], si[8];
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                *reinterpret_cast<float4*>(co + 4 * w) = *reinterpret_cast<const float4*>(cs + c * 8 + 4 * w);
-                *reinterpret_cast<float4*>(si + 4 * w) = *reinterpret_cast<const float4*>(sn + c * 8 + 4 * w);
-            }
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const float2 a = Half<T>::up(wl[w]), b = Half<T>::up(wh[w]);
-                const float c0 = co[2 * w], c1 = co[2 * w + 1], s0 = si[2 * w], s1 = si[2 * w + 1];
-                wl[w] = Half<T>::down(__fsub_rn(__fmul_rn(a.x, c0), __fmul_rn(b.x, s0)), __fsub_rn(__fmul_rn(a.y, c1), __fmul_rn(b.y, s1)));
-                wh[w] = Half<T>::down(__fadd_rn(__fmul_rn(b.x, c0), __fmul_rn(a.x, s0)), __fadd_rn(__fmul_rn(b.y, c1), __fmul_rn(a.y, s1)));
-            }
-        } else {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                float co[4], si[4];
-                *reinterpret_cast<float4*>(co) = *reinterpret_cast<const float4*>(cs + c * 4 + u * (D / 4));
-                *reinterpret_cast<float4*>(si) = *reinterpret_cast<const float4*>(sn + c * 4 + u * (D / 4));
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const float2 x = Half<T>::up(u ? wh[w] : wl[w]);
-                    const uint32_t y = Half<T>::down(__fsub_rn(__fmul_rn(x.x, co[w]), __fmul_rn(x.y, si[w])),
-                                                     __fadd_rn(__fmul_rn(x.y, co[w]), __fmul_rn(x.x, si[w])));
-                    if (u) wh[w] = y; else wl[w] = y;
-                }
-            }
-        }
-        lo = make_uint4(wl[0], wl[1], wl[2], wl[3]);
-        hi = make_uint4(wh[0], wh[1], wh[2], wh[3]);
-    }
-    if (kind == 2) {
-        if (ok) {
-            char* dst = p.q_out + ((size_t)token * p.H + head) * (D * 2) + c * 16;
-            *reinterpret_cast<uint4*>(dst) = lo;
-            *reinterpret_cast<uint4*>(dst + D) = hi;
-        }
-    } else if (BITS == 16) {
-        if (ok) {
-            char* dst = (kind == 0 ? p.kp : p.vp) + (size_t)(at.row + ((long long)head << p.t.page_log)) * (D * 2) + c * 16;
-            *reinterpret_cast<uint4*>(dst) = lo;
-            *reinterpret_cast<uint4*>(dst + D) = hi;
-        }
-    }
-    if (BITS == 4) {                                          // (every thread: the row's threads exchange)
-        if (!__any_sync(0xffffffffu, ok && kind != 2)) return;
-        float x[16];
-        const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-        uint32_t bad = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float2 f = Half<T>::up(w[e]);
-            x[2 * e] = f.x;
-            x[2 * e + 1] = f.y;
-            if ((w[e] & 0x7FFFu) >= Half<T>::kInf) bad |= 1u << ((2 * e) & 3);
-            if (((w[e] >> 16) & 0x7FFFu) >= Half<T>::kInf) bad |= 1u << ((2 * e + 1) & 3);
-        }
-        float mn[4], mx[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            mn[j] = fminf(fminf(x[j], x[j + 4]), fminf(x[j + 8], x[j + 12]));
-            mx[j] = fmaxf(fmaxf(x[j], x[j + 4]), fmaxf(x[j + 8], x[j + 12]));
-        }
-#pragma unroll
-        for (int o = 1; o < TPR; o <<= 1) {
-            bad |= __shfl_xor_sync(0xffffffffu, bad, o);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                mn[j] = fminf(mn[j], __shfl_xor_sync(0xffffffffu, mn[j], o));
-                mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], o));
-            }
-        }
-        if (!ok || kind == 2) return;
-        float s[4], z[4];
-        uint32_t sw[2], zw[2];
-        {
-            float st[4], zt[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                st[j] = __fmul_rn(__fsub_rn(mx[j], mn[j]), 0x1.111112p-4f);       // 1/15, rounded
-                zt[j] = __fadd_rn(mn[j], 8.f * st[j]);
-            }
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                sw[j] = Half<T>::down(st[2 * j], st[2 * j + 1]);
-                zw[j] = Half<T>::down(zt[2 * j], zt[2 * j + 1]);
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {                 // a range that the type cannot hold is not held at all either
-                    const uint32_t m = 0x7FFFu << (16 * u), inf = Half<T>::kInf << (16 * u);
-                    if ((bad >> (2 * j + u) & 1u) || (sw[j] & m) >= inf || (zw[j] & m) >= inf) {
-                        sw[j] |= Half<T>::kNan << (16 * u);
-                        zw[j] |= Half<T>::kNan << (16 * u);
-                        bad |= 1u << (2 * j + u);
-                    }
-                }
-                const float2 a = Half<T>::up(sw[j]), b = Half<T>::up(zw[j]);
-                s[2 * j] = a.x; s[2 * j + 1] = a.y;
-                z[2 * j] = b.x; z[2 * j + 1] = b.y;
-            }
-        }
-        const float inv[4] = {1.f / s[0], 1.f / s[1], 1.f / s[2], 1.f / s[3]};
-        uint32_t code[2] = {0u, 0u};
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int j = e & 3;
-            int cd = 8;
-            if (s[j] > 0.f && !(bad >> j & 1u)) {
-                // the quotient by a reciprocal, good to 2^-21 of it; where it stands that near a tie, by a division.  (Far outside the
-                // range, where z's rounding is all there is, it may be large: clamped before it is an integer.)
-                const float y = __fsub_rn(x[e], z[j]);
-                float r = y * inv[j], w1 = rintf(r);
-                if (fabsf(fabsf(r - w1) - 0.5f) < 1e-4f) w1 = rintf(__fdiv_rn(y, s[j]));
-                cd = __float2int_rn(fminf(fmaxf(w1 + 8.f, 0.f), 15.f));
-            }
-            code[e >> 3] |= (uint32_t)cd << (4 * (e & 7));
-        }
-        const int ps = 1 << p.t.page_log;
-        const long long first = at.row + ((long long)head << p.t.page_log);          // row among all rows of the pool
-        const int in_page = (int)(first & (ps - 1));
-        char* blk = (kind == 0 ? p.kp : p.vp) + (size_t)(first >> p.t.page_log) * ((size_t)ps * (D / 2 + 16));
-        uint32_t* dst = reinterpret_cast<uint32_t*>(blk + (size_t)in_page * (D / 2));
-        dst[c] = code[0];
-        dst[c + D / 16] = code[1];
-        if (c == 0) *reinterpret_cast<uint4*>(blk + (size_t)ps * (D / 2) + in_page * 16) = make_uint4(sw[0], sw[1], zw[0], zw[1]);
-    }
+// A pair of rows' halves turned: (a, b) -> (a cos - b sin, b cos + a sin), products and sums rounded one by one (no contraction), so
+// that the stored value is the one that the formula gives in plain fp32 arithmetic: a code of the 4-bit form depends on its last bit.
+__device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
+    const float x = __fsub_rn(__fmul_rn(a, c), __fmul_rn(b, s));
+    b = __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
+    a = x;
 }
 
-// One row of head_dim values by D/16 threads, each with eight values of the lower half and the eight that stand D/2 behind them,
-// so that a thread holds whole pairs of either rotary style and two whole code words.
-//
-// Rotation: products and sums rounded one by one (no contraction), so that the stored value is the one that the formula gives in
-// plain fp32 arithmetic: a code of the 4-bit form depends on its last bit.
-// 4 bits: the four interleaved groups' extremes go round the row's threads by shuffles (log2(D/16) steps of eight); a thread's
-// eight neighbouring channels are one 32-bit word of codes.
-// A CTA takes up to 16 tokens and some or all of their rows, neighbouring thread groups the same head of neighbouring tokens, whose
-// page rows lie side by side; a token's page and its angles are fetched once, into shared memory.  Padding is not read.
+// Sixteen values of one row (eight channels from 8c, eight from D/2 + 8c) to codes; the row's other threads are the neighbouring lanes.
+// scales: the row's eight 16-bit values.  In 16-bit pairs a word holds groups 0 and 1 or groups 2 and 3, so the extremes are packed.
+template <typename T, int D>
+__device__ __forceinline__ void quantise(const uint32_t (&w)[8], uint32_t (&code)[2], uint4* scales) {
+    constexpr int TPR = D / 16;
+    using H = Half<T>;
+    uint32_t mn[2], mx[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        mn[j] = H::least(H::least(w[j], w[j + 2]), H::least(w[j + 4], w[j + 6]));
+        mx[j] = H::most(H::most(w[j], w[j + 2]), H::most(w[j + 4], w[j + 6]));
+    }
+#pragma unroll
+    for (int o = 1; o < TPR; o <<= 1) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            mn[j] = H::least(mn[j], __shfl_xor_sync(0xffffffffu, mn[j], o));
+            mx[j] = H::most(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], o));
+        }
+    }
+    uint32_t sw[2], zw[2];
+    float s[4], z[4], inv[4];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const float2 lo = H::up(mn[j]), hi = H::up(mx[j]);
+        const float a = __fmul_rn(__fsub_rn(hi.x, lo.x), 0x1.111112p-4f), b = __fmul_rn(__fsub_rn(hi.y, lo.y), 0x1.111112p-4f);   // 1/15, rounded
+        sw[j] = H::down(a, b);
+        zw[j] = H::down(__fadd_rn(lo.x, 8.f * a), __fadd_rn(lo.y, 8.f * b));
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {                         // Inf, NaN, or a range that the type cannot hold: not held
+            const uint32_t m = 0x7FFFu << (16 * u), inf = H::kInf << (16 * u);
+            if ((sw[j] & m) >= inf || (zw[j] & m) >= inf) {
+                sw[j] |= H::kNan << (16 * u);
+                zw[j] |= H::kNan << (16 * u);
+            }
+        }
+        const float2 x = H::up(sw[j]), y = H::up(zw[j]);
+        s[2 * j] = x.x; s[2 * j + 1] = x.y;
+        z[2 * j] = y.x; z[2 * j + 1] = y.y;
+        inv[2 * j] = x.x > 0.f ? 1.f / x.x : 0.f;             // (0 and NaN: every code is 8)
+        inv[2 * j + 1] = x.y > 0.f ? 1.f / x.y : 0.f;
+    }
+    // code = rint((x - z)/s) + 8, clamped.  The quotient is a product with the reciprocal, good to 2^-21 of it; adding 1.5 * 2^23 rounds
+    // it (ties to even) and leaves the code in the low bits.  Where it stands within 2e-5 of a tie the row's words are done again
+    // by division.  (Far outside the range, where z's rounding is all there is, the quotient may be large: the clamp is before the bits.)
+    constexpr float kRound = 12582912.f;
+    bool near = false;
+    code[0] = code[1] = 0u;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const float2 f = H::up(w[e >> 1]);
+        const float i = inv[e & 3], y = i > 0.f ? __fsub_rn(e & 1 ? f.y : f.x, z[e & 3]) : 0.f;
+        const float r = fmaf(y, i, kRound + 8.f);
+        near |= fabsf(fmaf(y, i, kRound + 8.f - r)) > 0.49998f;
+        code[e >> 3] += __float_as_uint(fminf(fmaxf(r, kRound), kRound + 15.f)) << (4 * (e & 7));
+    }
+    if (near) {
+        code[0] = code[1] = 0u;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float2 f = H::up(w[e >> 1]);
+            const float i = inv[e & 3], y = __fsub_rn(e & 1 ? f.y : f.x, z[e & 3]);
+            const float r = i > 0.f ? __fdiv_rn(y, s[e & 3]) : 0.f;
+            code[e >> 3] += __float_as_uint(fminf(fmaxf(r + (kRound + 8.f), kRound), kRound + 15.f)) << (4 * (e & 7));
+        }
+    }
+    constexpr uint32_t kBits = 0x4B400000u;                   // of kRound: what the eight sums have too much (the rest has left at the top)
+    code[0] -= kBits + (kBits << 4) + (kBits << 8);
+    code[1] -= kBits + (kBits << 4) + (kBits << 8);
+    *scales = make_uint4(sw[0], sw[1], zw[0], zw[1]);
+}
+
+// A row of head_dim values by D/16 threads, each with eight values of the lower half and the eight that stand D/2 behind them,
+// so that a thread holds whole pairs of either rotary style and two whole code words.  A CTA takes up to 8 tokens and some or all of
+// their rows; a thread stays with one token and goes through its rows, so that the token's page is looked up, and its angles are
+// fetched, once.  Neighbouring thread groups have neighbouring tokens, whose page rows lie side by side.  Padding is not read.
 // Bound: HBM for prompts (each value in once, each row out once), the chain length -> page -> store for a single token.
 template <typename T, int D, int BITS, int STYLE>
-__global__ void __launch_bounds__(kThreads) pages_append_kernel(const __grid_constant__ AppendParams p) {
+__global__ void __launch_bounds__(kThreads, BITS == 16 ? 4 : 3) pages_append_kernel(const __grid_constant__ AppendParams p) {
     constexpr int TPR = D / 16, SLOTS = kThreads / TPR;
     __shared__ Place s_place[kTokenBlock];
-    __shared__ __align__(16) float s_cos[STYLE ? kTokenBlock * (D / 2) : 4], s_sin[STYLE ? kTokenBlock * (D / 2) : 4];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int c = threadIdx.x % TPR, slot = threadIdx.x / TPR;
+    const int tl = slot & ((1 << p.t.block_log) - 1), rl = slot >> p.t.block_log, rs = SLOTS >> p.t.block_log;
+    const int token = (blockIdx.x << p.t.block_log) + tl;
+    const int row0 = blockIdx.y * p.t.rows_cta, row1 = min(row0 + p.t.rows_cta, p.t.rows);
+    const int Hkv = p.t.Hkv;
+    const size_t head_bytes = (size_t)((D * 2) << p.t.page_log);                       // 16 bits: of one head's rows in a page
+    // key, value and query rows are numbered through: row r of the token is at base + r rows
+    const char* const src_k = p.k + (long long)token * p.k_stride + c * 16;
+    const char* const src_v = p.v + (long long)token * p.v_stride + c * 16 - (size_t)Hkv * (D * 2);
+    const char* const src_q = p.q + (long long)token * p.q_stride + c * 16 - (size_t)2 * Hkv * (D * 2);
+    constexpr int AHEAD = 2;
+    uint4 lo[AHEAD], hi[AHEAD];                               // the next rows
+    auto fetch = [&](uint4& lo, uint4& hi, int row, bool real) {
+        lo = hi = make_uint4(0u, 0u, 0u, 0u);
+        if (real && row < row1) {
+            const char* src = (row < Hkv ? src_k : row < 2 * Hkv ? src_v : src_q) + (size_t)row * (D * 2);
+            lo = *reinterpret_cast<const uint4*>(src);
+            hi = *reinterpret_cast<const uint4*>(src + D);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) fetch(lo[i], hi[i], row0 + rl + i * rs, token < p.t.tokens);      // (before it is known whether it is padding, which is there to be read)
     find_places(p.t, s_place, STYLE ? p.positions : 0x7FFFFFFF, false);
     __syncthreads();
-    if (STYLE) {
-        for (int i = threadIdx.x; i < (D / 2) << p.t.block_log; i += kThreads) {
-            const Place a = s_place[i / (D / 2)];
-            if (a.row >= 0) {
-                s_cos[i] = __ldg(p.cos + (size_t)a.pos * (D / 2) + i % (D / 2));
-                s_sin[i] = __ldg(p.sin + (size_t)a.pos * (D / 2) + i % (D / 2));
-            }
+    const Place at = s_place[tl];
+    const bool real = at.row >= 0;
+    float co[8], si[8];
+    if (STYLE != 0 && real) {
+        const float* cs = p.cos + (size_t)at.pos * (D / 2);
+        const float* sn = p.sin + (size_t)at.pos * (D / 2);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {                         // interleaved: pairs 4c .. of the lower half, then of the upper
+            const int i = STYLE == SEGKV_ROPE_HALF ? c * 8 + e : c * 4 + (e & 3) + (e >> 2) * (D / 4);
+            co[e] = __ldg(cs + i);
+            si[e] = __ldg(sn + i);
         }
-        __syncthreads();
     }
-    const int c = threadIdx.x % TPR, slot = threadIdx.x / TPR;
-    const int row0 = blockIdx.y * p.t.rows_cta, rows = min(p.t.rows_cta, p.t.rows - row0);
-    const int items = rows << p.t.block_log;
-    const int tok0 = blockIdx.x << p.t.block_log;
-    constexpr int U = 2;                                      // rows of a thread in flight
-    for (int i0 = 0; i0 < items; i0 += U * SLOTS) {
-        uint4 lo_[U], hi_[U];
+    char* const dst_q = p.q_out + ((size_t)token * p.H) * (D * 2) + c * 16 - (size_t)2 * Hkv * (D * 2);
+    const int ps = 1 << p.t.page_log, in_page = (int)(at.row & (ps - 1));
+    const size_t block = (size_t)ps * (D / 2 + 16);                                    // 4 bits: bytes of one head's rows in a page
+    const size_t at_bytes = BITS == 16 ? (size_t)at.row * (D * 2) + c * 16 : (size_t)(at.row >> p.t.page_log) * block;
+
+    for (int r0 = row0; r0 < row1; r0 += rs) {
+        const int row = r0 + rl;
+        uint32_t w[8] = {lo[0].x, lo[0].y, lo[0].z, lo[0].w, hi[0].x, hi[0].y, hi[0].z, hi[0].w};
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = i0 + u * SLOTS + slot, tl = i & ((1 << p.t.block_log) - 1), row = row0 + (i >> p.t.block_log);
-            lo_[u] = hi_[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (i < items && s_place[tl].row >= 0) {
-                const long long token = tok0 + tl;
-                const char* src = row < p.t.Hkv ? p.k + token * p.k_stride + (size_t)row * (D * 2)
-                                  : row < 2 * p.t.Hkv ? p.v + token * p.v_stride + (size_t)(row - p.t.Hkv) * (D * 2)
-                                                      : p.q + token * p.q_stride + (size_t)(row - 2 * p.t.Hkv) * (D * 2);
-                lo_[u] = *reinterpret_cast<const uint4*>(src + c * 16);
-                hi_[u] = *reinterpret_cast<const uint4*>(src + c * 16 + D);
+        for (int i = 0; i + 1 < AHEAD; ++i) {
+            lo[i] = lo[i + 1];
+            hi[i] = hi[i + 1];
+        }
+        fetch(lo[AHEAD - 1], hi[AHEAD - 1], row + AHEAD * rs, real);
+        const bool ok = real && row < row1;
+        const bool is_q = row >= 2 * Hkv, is_v = row >= Hkv && !is_q;
+        if (STYLE != 0 && !is_v) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float2 a = Half<T>::up(w[e]), b = Half<T>::up(w[e + 4]);
+                if (STYLE == SEGKV_ROPE_HALF) {
+                    turn(a.x, b.x, co[2 * e], si[2 * e]);
+                    turn(a.y, b.y, co[2 * e + 1], si[2 * e + 1]);
+                } else {
+                    turn(a.x, a.y, co[e], si[e]);
+                    turn(b.x, b.y, co[e + 4], si[e + 4]);
+                }
+                w[e] = Half<T>::down(a.x, a.y);
+                w[e + 4] = Half<T>::down(b.x, b.y);
             }
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (i0 + u * SLOTS >= items) break;               // (every thread)
-            const int i = i0 + u * SLOTS + slot, tl = i & ((1 << p.t.block_log) - 1), row = row0 + (i >> p.t.block_log);
-            const Place at = s_place[tl];
-            const bool ok = i < items && at.row >= 0;
-            const int kind = row < p.t.Hkv ? 0 : row < 2 * p.t.Hkv ? 1 : 2;            // key, value, query
-            const int head = row - kind * p.t.Hkv;
-            store_row<T, D, BITS, STYLE>(p, at, ok, kind, head, tok0 + tl, c, lo_[u], hi_[u], s_cos + tl * (D / 2), s_sin + tl * (D / 2));
+        char* const pages = is_v ? p.vp : p.kp;
+        const int head = is_v ? row - Hkv : row;
+        if (BITS == 16 || is_q) {
+            char* dst = is_q ? dst_q + (size_t)row * (D * 2) : pages + at_bytes + (size_t)head * head_bytes;
+            if (ok) {
+                *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4*>(dst + D) = make_uint4(w[4], w[5], w[6], w[7]);
+            }
+        }
+        if (BITS == 4) {
+            if (!__any_sync(0xffffffffu, ok && !is_q)) continue;                       // (every thread else: the row's threads exchange)
+            uint32_t code[2];
+            uint4 scales;
+            quantise<T, D>(w, code, &scales);
+            if (ok && !is_q) {
+                char* blk = pages + at_bytes + (size_t)head * block;
+                uint32_t* dst = reinterpret_cast<uint32_t*>(blk + (size_t)in_page * (D / 2));
+                dst[c] = code[0];
+                dst[c + D / 16] = code[1];
+                if (c == 0) *reinterpret_cast<uint4*>(blk + (size_t)ps * (D / 2) + in_page * 16) = scales;
+            }
         }
     }
 }
@@ -299,7 +302,7 @@ struct ReadParams {
     char *k, *v;
 };
 
-// Eight neighbouring values of a row per thread, a CTA's tokens and rows as in the append.  Bound: HBM.
+// Eight neighbouring values of a row per thread, tokens and rows dealt as in the append.  Bound: HBM.
 template <typename T, int D, int BITS>
 __global__ void __launch_bounds__(kThreads) pages_read_kernel(const __grid_constant__ ReadParams p) {
     constexpr int TPR = D / 8, SLOTS = kThreads / TPR;
@@ -309,37 +312,37 @@ __global__ void __launch_bounds__(kThreads) pages_read_kernel(const __grid_const
     find_places(p.t, s_place, 0x7FFFFFFF, true);
     __syncthreads();
     const int c = threadIdx.x % TPR, slot = threadIdx.x / TPR;
-    const int row0 = blockIdx.y * p.t.rows_cta, rows = min(p.t.rows_cta, p.t.rows - row0);
-    const int items = rows << p.t.block_log;
-    const int tok0 = blockIdx.x << p.t.block_log;
-    const int ps = 1 << p.t.page_log;
+    const int tl = slot & ((1 << p.t.block_log) - 1), rl = slot >> p.t.block_log, rs = SLOTS >> p.t.block_log;
+    const int token = (blockIdx.x << p.t.block_log) + tl;
+    const int row1 = min((int)(blockIdx.y + 1) * p.t.rows_cta, p.t.rows);
+    const int Hkv = p.t.Hkv;
+    const Place at = s_place[tl];
+    if (at.row < 0) return;
+    const int ps = 1 << p.t.page_log, in_page = (int)(at.row & (ps - 1));
+    const size_t block = (size_t)ps * (BITS == 16 ? D * 2 : D / 2 + 16);               // of one head's rows in a page
+    const size_t at_bytes = (size_t)(at.row >> p.t.page_log) * block + (size_t)in_page * (BITS == 16 ? D * 2 : D / 2);
+    char* const dst_k = p.k + (size_t)token * Hkv * (D * 2) + c * 16;
+    char* const dst_v = p.v + (size_t)token * Hkv * (D * 2) + c * 16 - (size_t)Hkv * (D * 2);
     constexpr int U = 4;                                      // rows of a thread in flight
-    for (int i0 = 0; i0 < items; i0 += U * SLOTS) {
+    for (int r0 = blockIdx.y * p.t.rows_cta + rl; r0 < row1; r0 += U * rs) {
         uint4 x[U];
         uint32_t code[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int i = i0 + u * SLOTS + slot, tl = i & ((1 << p.t.block_log) - 1), row = row0 + (i >> p.t.block_log);
-            x[u] = make_uint4(0u, 0u, 0u, 0u);
-            code[u] = 0u;
-            if (i >= items || s_place[tl].row < 0) continue;
-            const int kind = row < p.t.Hkv ? 0 : 1, head = row - kind * p.t.Hkv;
-            const long long first = s_place[tl].row + ((long long)head << p.t.page_log);
-            const char* pages = kind == 0 ? p.kp : p.vp;
+            const int row = r0 + u * rs;
+            if (row >= row1) break;
+            const char* blk = (row < Hkv ? p.kp : p.vp) + at_bytes + (size_t)(row < Hkv ? row : row - Hkv) * block;
             if (BITS == 16) {
-                x[u] = *reinterpret_cast<const uint4*>(pages + (size_t)first * (D * 2) + c * 16);
+                x[u] = *reinterpret_cast<const uint4*>(blk + c * 16);
             } else {
-                const int in_page = (int)(first & (ps - 1));
-                const char* blk = pages + (size_t)(first >> p.t.page_log) * ((size_t)ps * (D / 2 + 16));
-                code[u] = reinterpret_cast<const uint32_t*>(blk + (size_t)in_page * (D / 2))[c];
-                x[u] = *reinterpret_cast<const uint4*>(blk + (size_t)ps * (D / 2) + in_page * 16);
+                code[u] = *reinterpret_cast<const uint32_t*>(blk + c * 4);
+                x[u] = *reinterpret_cast<const uint4*>(blk + (size_t)ps * (D / 2) + in_page * (16 - D / 2));
             }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int i = i0 + u * SLOTS + slot, tl = i & ((1 << p.t.block_log) - 1), row = row0 + (i >> p.t.block_log);
-            if (i >= items || s_place[tl].row < 0) continue;
-            const int kind = row < p.t.Hkv ? 0 : 1, head = row - kind * p.t.Hkv;
+            const int row = r0 + u * rs;
+            if (row >= row1) break;
             uint4 out = x[u];
             if (BITS == 4) {
                 const float2 s0 = Half<T>::up(x[u].x), s1 = Half<T>::up(x[u].y), z0 = Half<T>::up(x[u].z), z1 = Half<T>::up(x[u].w);
@@ -349,21 +352,21 @@ __global__ void __launch_bounds__(kThreads) pages_read_kernel(const __grid_const
                 for (int e = 0; e < 8; ++e) v[e] = fmaf((float)((int)(code[u] >> (4 * e) & 15u) - 8), s4[e & 3], z4[e & 3]);
                 out = make_uint4(Half<T>::down(v[0], v[1]), Half<T>::down(v[2], v[3]), Half<T>::down(v[4], v[5]), Half<T>::down(v[6], v[7]));
             }
-            char* dst = (kind == 0 ? p.k : p.v) + ((size_t)(tok0 + tl) * p.t.Hkv + head) * (D * 2) + c * 16;
-            *reinterpret_cast<uint4*>(dst) = out;
+            *reinterpret_cast<uint4*>((row < Hkv ? dst_k : dst_v) + (size_t)row * (D * 2)) = out;
         }
     }
 }
 
 template <typename P>
-cudaError_t launch(void (*kernel)(P), P& p, int slots, int sm_count, bool pdl, cudaStream_t st) {
-    // tokens of a CTA: 16, fewer where there are fewer; rows of a CTA: all, or as many fewer as give the GPU four CTAs an SM, but
-    // one row for each of a CTA's thread groups at least
+cudaError_t launch(void (*kernel)(P), P& p, int slots, int sm_count, int per_sm, bool pdl, cudaStream_t st) {
+    // tokens of a CTA: 8, fewer where there are fewer or a CTA's threads make fewer rows; of their rows, rs at a time, as many rounds as leave the GPU per_sm CTAs an SM
     p.t.block_log = 0;
-    while ((1 << p.t.block_log) < kTokenBlock && (2 << p.t.block_log) <= p.t.tokens) p.t.block_log++;
+    while ((1 << p.t.block_log) < kTokenBlock && (2 << p.t.block_log) <= slots && (2 << p.t.block_log) <= p.t.tokens) p.t.block_log++;
     const long long blocks = ((long long)p.t.tokens + (1 << p.t.block_log) - 1) >> p.t.block_log;
-    int rows = p.t.rows;
-    while (rows > 1 && (rows << p.t.block_log) > slots && blocks * ((p.t.rows + rows - 1) / rows) < 4LL * sm_count) rows = (rows + 1) / 2;
+    const int rs = slots >> p.t.block_log;
+    int rounds = (p.t.rows + rs - 1) / rs;
+    while (rounds > 1 && blocks * ((p.t.rows + rounds * rs - 1) / (rounds * rs)) < (long long)per_sm * sm_count) rounds = (rounds + 1) / 2;
+    const int rows = rounds * rs;
     p.t.rows_cta = rows;
     const int chunks = (p.t.rows + rows - 1) / rows;
     if (chunks > 65535) return cudaErrorInvalidConfiguration;
@@ -416,7 +419,7 @@ cudaError_t launch_pages_append(const segkv_pages& h, const PageAppendArgs& a, c
     p.kp = h.kp; p.vp = h.vp; p.q_out = (char*)a.q_out;
     p.cos = a.cos; p.sin = a.sin; p.H = h.heads; p.positions = a.positions;
     auto kernel = h.dtype == SEGKV_BF16 ? append_of<__nv_bfloat16>(h.head_dim, h.bits, a.style) : append_of<__half>(h.head_dim, h.bits, a.style);
-    return launch(kernel, p, kThreads / (h.head_dim / 16), h.sm_count, a.t.pdl, st);
+    return launch(kernel, p, kThreads / (h.head_dim / 16), h.sm_count, 8, a.t.pdl, st);
 }
 
 cudaError_t launch_pages_read(const segkv_pages& h, const PageTokens& t, void* k_out, void* v_out, cudaStream_t st) {
@@ -424,7 +427,7 @@ cudaError_t launch_pages_read(const segkv_pages& h, const PageTokens& t, void* k
     p.t = token_params(h, t, 2 * h.kv_heads);
     p.kp = h.kp; p.vp = h.vp; p.k = (char*)k_out; p.v = (char*)v_out;
     auto kernel = h.dtype == SEGKV_BF16 ? read_of<__nv_bfloat16>(h.head_dim, h.bits) : read_of<__half>(h.head_dim, h.bits);
-    return launch(kernel, p, kThreads / (h.head_dim / 8), h.sm_count, t.pdl, st);
+    return launch(kernel, p, kThreads / (h.head_dim / 8), h.sm_count, 8, t.pdl, st);
 }
 
 }  // namespace segkv_impl

@@ -1,6 +1,7 @@
 """Thin binding of the paged cache (``include/segkv_pages.h``): keys and values of requests that come and go, in pages of 16 or 4 bits.
 
-Argument marshalling only, as in :mod:`.segkv`; every step runs in the library's CUDA kernels.
+Argument marshalling only, as in :mod:`.segkv`; every step runs in the library's CUDA kernels.  Calls whose arguments are plainly what
+is expected are checked and made in the extension module, the others here.
 """
 from __future__ import annotations
 
@@ -9,7 +10,7 @@ from typing import Optional
 
 import torch
 
-from .segkv import SEGKV_BF16, SEGKV_F16, _check, _int, _stream_ptr, _vp, lib
+from .segkv import SEGKV_BF16, SEGKV_F16, _check, _hot_module, _int, _stream_ptr, _vp, lib
 
 
 def page_bytes(kv_heads: int, head_dim: int, page_size: int, num_pages: int, kv_bits: int = 16) -> int:
@@ -30,7 +31,7 @@ class PagedKV:
 
     def __init__(self, heads: int, kv_heads: int, head_dim: int, page_size: int, num_pages: int, dtype=torch.float16, kv_bits: int = 16,
                  k_pages: Optional[torch.Tensor] = None, v_pages: Optional[torch.Tensor] = None):
-        self._h = _vp()
+        self._h, self._hot = _vp(), None
         self.heads, self.kv_heads, self.head_dim = heads, kv_heads, head_dim
         self.page_size, self.num_pages, self.dtype, self.kv_bits = page_size, num_pages, dtype, kv_bits
         code = {torch.float16: SEGKV_F16, torch.bfloat16: SEGKV_BF16}.get(dtype, -1)
@@ -52,13 +53,16 @@ class PagedKV:
         with torch.cuda.device(self.device):
             _check(lib().segkv_pages_create(ctypes.byref(self._h), heads, kv_heads, head_dim, page_size, num_pages, code, kv_bits,
                                             k_pages.data_ptr(), v_pages.data_ptr()), "segkv_pages_create")
+        L, hot = lib(), _hot_module()
+        self._hot = None if not hasattr(hot, "Pages") else hot.Pages(self._h.value, heads, kv_heads, head_dim, self.device.index, dtype is torch.bfloat16, tuple(
+            ctypes.cast(f, ctypes.c_void_p).value for f in (L.segkv_pages_append, L.segkv_pages_sdpa, L.segkv_pages_read)))
 
     # ------------------------------------------------------------ life cycle
     def destroy(self) -> None:
         if getattr(self, "_h", None) is not None and self._h:
             with torch.cuda.device(self.device):
                 _check(lib().segkv_pages_destroy(self._h), "segkv_pages_destroy")
-            self._h = None
+            self._h = self._hot = None
 
     def __del__(self):
         try:
@@ -124,6 +128,14 @@ class PagedKV:
                rope_sin: Optional[torch.Tensor] = None, style="half", stream=None) -> Optional[torch.Tensor]:
         """segkv_pages_append.  k, v [n, tokens, kv_heads, head_dim], q [n, tokens, heads, head_dim] (slices of a packed projection
         will do); returns q_out, made here if it is not given."""
+        if stream is None and self._hot is not None:
+            if q is not None and q_out is None:
+                q_out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+            rc = self._hot.append(k, v, table, lens, new_lens, q, q_out, rope_cos, rope_sin, self.ROPE_STYLES.get(style, style))
+            if rc == 0:
+                return q_out
+            if rc is not None:
+                _check(rc, "segkv_pages_append")
         n, entries = self._index(table, lens, new_lens)
         tokens = k.shape[1] if k.dim() == 4 else -1
         if v.dim() != 4 or v.shape[1] != tokens or (q is not None and (q.dim() != 4 or q.shape[1] != tokens)):
@@ -157,6 +169,14 @@ class PagedKV:
     def sdpa(self, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, out: Optional[torch.Tensor] = None,
              alibi_slopes: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """segkv_pages_sdpa.  q, out [n, q_len, heads, head_dim]: the newest q_len tokens of every sequence."""
+        if stream is None and self._hot is not None:
+            if out is None:
+                out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+            rc = self._hot.sdpa(q, table, lens, out, alibi_slopes)
+            if rc == 0:
+                return out
+            if rc is not None:
+                _check(rc, "segkv_pages_sdpa")
         n, entries = self._index(table, lens, None)
         qp, qs = self._rows(q, n, self.heads, "q")
         if out is None:
@@ -176,10 +196,16 @@ class PagedKV:
     def read(self, table: torch.Tensor, lens: torch.Tensor, tokens: int, new_lens: Optional[torch.Tensor] = None,
              k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None, stream=None):
         """segkv_pages_read: (k, v) [n, tokens, kv_heads, head_dim], made here (zeros) if they are not given."""
-        n, entries = self._index(table, lens, new_lens)
-        shape = (n, tokens, self.kv_heads, self.head_dim)
+        shape = (lens.shape[0], tokens, self.kv_heads, self.head_dim)
         k = torch.zeros(shape, dtype=self.dtype, device=self.device) if k is None else k
         v = torch.zeros(shape, dtype=self.dtype, device=self.device) if v is None else v
+        if stream is None and self._hot is not None:
+            rc = self._hot.read(table, lens, tokens, new_lens, k, v)
+            if rc == 0:
+                return k, v
+            if rc is not None:
+                _check(rc, "segkv_pages_read")
+        n, entries = self._index(table, lens, new_lens)
         kp, vp = self._dense(k, shape, "k"), self._dense(v, shape, "v")
         rc = lib().segkv_pages_read(self._h, n, tokens, kp, vp, table.data_ptr(), entries, lens.data_ptr(),
                                     None if new_lens is None else new_lens.data_ptr(), self._stream(stream))

@@ -528,3 +528,20 @@ def test_refused_arguments():
     c.destroy()
     with pytest.raises(sk.SegKVError):
         c.sdpa(q, table, lens)
+
+
+def test_calls_with_a_stream_argument_take_the_general_path():
+    """The same calls through the extension module and through ctypes: what one takes the other takes, with the same bits."""
+    c, table, lens = filled(4, 2, 64, 16, [30, 40], F16, 4, 181)
+    st = torch.cuda.current_stream()
+    q, k, v = packed(2, 2, 4, 2, 64, F16, 182)
+    cos, sin = (x.cuda() for x in wl.rope_tables(64, 64))
+    new = torch.tensor([2, 1], dtype=torch.int32, device="cuda")
+    got = []
+    for stream in (None, st):
+        qr = c.append(k, v, table, lens, new, q=q, q_out=torch.zeros(2, 2, 4, 64, dtype=F16, device="cuda"), rope_cos=cos, rope_sin=sin,
+                      style="interleaved", stream=stream)
+        got.append([qr, c.sdpa(qr, table, lens, None, wl.alibi_slopes(4).cuda(), stream=stream), *c.read(table, lens, 3, new, stream=stream)])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert c._hot is None or c._hot.sdpa(q.float(), table, lens, got[0][1], None) is None       # not its to take
+    c.destroy()
