@@ -64,31 +64,14 @@ EncodeTiledFn encode_tiled_fn() {
     return fn;
 }
 
-// A 4-D tensor map in coordinates (d, head, token, request) over 16-bit elements: `heads` heads,
+// A map (encode_map) with the handle's type, head size and requests: `heads` heads,
 // `tokens` tokens (those past the extent read as zero), element strides of a head / token /
 // request as given, box = 64 elements (128 bytes, one swizzle span) x box_tokens tokens of one
 // (request, head), 128-byte swizzle.  `what` names the array in the error text.
 int encode_map_4d(const segkv* h, const void* base, int heads, int tokens, long long stride_h, long long stride_p,
                   long long stride_b, int box_tokens, const char* what, CUtensorMap* out) {
-    EncodeTiledFn fn = encode_tiled_fn();
-    if (!fn) {
-        snprintf(g_cuda_err, sizeof g_cuda_err, "cuTensorMapEncodeTiled entry point not available");
-        return SEGKV_ECUDA;
-    }
     const Dims& d = h->d;
-    cuuint64_t dims[4] = {(cuuint64_t)d.head_dim, (cuuint64_t)heads, (cuuint64_t)tokens, (cuuint64_t)d.batch};
-    cuuint64_t strides[3] = {(cuuint64_t)stride_h * 2, (cuuint64_t)stride_p * 2, (cuuint64_t)stride_b * 2};
-    cuuint32_t box[4] = {64, 1, (cuuint32_t)box_tokens, 1};
-    cuuint32_t estr[4] = {1, 1, 1, 1};
-    CUtensorMapDataType dt = d.dtype == SEGKV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    CUresult r = fn(out, dt, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) {
-        snprintf(g_cuda_err, sizeof g_cuda_err, "cuTensorMapEncodeTiled (%s) failed with CUresult %d", what, (int)r);
-        return SEGKV_ECUDA;
-    }
-    return SEGKV_OK;
+    return encode_map(base, d.dtype == SEGKV_BF16, d.head_dim, heads, tokens, d.batch, stride_h, stride_p, stride_b, 1, box_tokens, what, out);
 }
 
 // One prompt array of the handle, [batch][prompt_len][kv_heads][D] logically, with the strides
@@ -529,6 +512,27 @@ SdpaArgs sdpa_args(const segkv* h, const void* q, void* out, const float* slopes
 }  // namespace
 
 namespace segkv_impl {
+int encode_map(const void* base, bool bf16, int head_dim, int heads, int tokens, int requests, long long stride_h, long long stride_p,
+               long long stride_b, int box_heads, int box_tokens, const char* what, CUtensorMap* out) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) {
+        snprintf(g_cuda_err, sizeof g_cuda_err, "cuTensorMapEncodeTiled entry point not available");
+        return SEGKV_ECUDA;
+    }
+    cuuint64_t dims[4] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)tokens, (cuuint64_t)requests};
+    cuuint64_t strides[3] = {(cuuint64_t)stride_h * 2, (cuuint64_t)stride_p * 2, (cuuint64_t)stride_b * 2};
+    cuuint32_t box[4] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_tokens, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    CUtensorMapDataType dt = bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    CUresult r = fn(out, dt, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        snprintf(g_cuda_err, sizeof g_cuda_err, "cuTensorMapEncodeTiled (%s) failed with CUresult %d", what, (int)r);
+        return SEGKV_ECUDA;
+    }
+    return SEGKV_OK;
+}
 // for the paged cache (segkv_pages_api.cu): errors in the library's manner, launches in the order of its streams
 int report_cuda(cudaError_t e, const char* what) { return cuda_fail(e, what); }
 void log_launch(int device, cudaStream_t st, Release rel) { g_log.note(stream_key(device, st), rel); }

@@ -232,7 +232,15 @@ struct PrefillArgs {
     bool pdl;            // launch with programmatic stream serialisation
     unsigned long long wait_ns;   // test aid, as in SdpaArgs
     bool dbg_skip;
+    // pages instead of a prompt segment (table not NULL): tm_k and tm_v are maps of the pool; prompt_len, and heads, kv_heads and group of the
+    // dims, count packed rows and groups of packed heads (see the kernel)
+    const int32_t *table = nullptr, *lens = nullptr;
+    int table_stride = 0, page_log = 0, num_pages = 0, q_len = 0, pack_log = 0, box_log = 0;
 };
+// A 4-D tensor map over 16-bit elements in coordinates (d, head, token, request): extents, element strides of the last three, box
+// in heads and tokens (and 64 elements: one 128-byte swizzle span).  `what` names the array in the error text.
+int encode_map(const void* base, bool bf16, int head_dim, int heads, int tokens, int requests, long long stride_h, long long stride_p,
+               long long stride_b, int box_heads, int box_tokens, const char* what, CUtensorMap* out);
 // tcgen05 tensor cores with TMEM accumulators; head_dim 64, 128 or 256
 bool prefill_tc5_supported(const Dims& d);
 cudaError_t launch_prefill_tc5(const Dims& d, const PrefillArgs& a, cudaStream_t st);

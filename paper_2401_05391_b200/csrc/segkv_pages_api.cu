@@ -1,4 +1,5 @@
 // Host side of the paged cache: handle life cycle, argument checks, launches.
+#include <stdlib.h>
 #include <string.h>
 
 #include <new>
@@ -41,6 +42,21 @@ int launched(segkv_pages* h, cudaError_t e, const char* what, void* stream) {
     h->launches++;
     log_launch(h->device, (cudaStream_t)stream, kAfterWait);
     return SEGKV_OK;
+}
+
+// How many query heads of a kv head stand side by side in the rows of the tensor-core kernel, as a power of two: as many as divide the
+// group; one where each has a slope of its own.
+int pack_log(const segkv_pages* h, bool slopes) {
+    int g = 0;
+    while (!slopes && g < 5 && h->group % (2 << g) == 0) ++g;
+    return g;
+}
+
+// Does the tensor-core kernel serve the call?
+bool many_rows(const segkv_pages* h, int n, int q_len, int pack) {
+    if (h->bits != 16) return false;
+    static const char* x = getenv("SEGKV_X");
+    return x ? atoi(x) != 0 : (long long)q_len << pack >= 128;
 }
 
 void free_all(segkv_pages* h) {
@@ -91,6 +107,19 @@ int segkv_pages_create(segkv_pages_t* out, int heads, int kv_heads, int head_dim
     SEGKV_TRY(cudaMemset(h->tickets, 0, grid * sizeof(int)));
     SEGKV_TRY(cudaMemset(h->err_word, 0, sizeof(int)));
 #undef SEGKV_TRY
+    if (kv_bits == 16) {
+        // for the tensor-core kernel of many query rows: a copy brings the rows of one page, or of one of its tiles
+        const int tile = head_dim == 256 ? 64 : 128, box = page_size < tile ? page_size : tile;
+        while ((1 << h->box_log) < box) h->box_log++;
+        const long long D = head_dim, ps = page_size;
+        int rc = encode_map(k_pages, dtype == SEGKV_BF16, head_dim, kv_heads, page_size, num_pages, ps * D, D, kv_heads * ps * D, 1, box, "K pages", &h->tm_k);
+        if (rc == SEGKV_OK) rc = encode_map(v_pages, dtype == SEGKV_BF16, head_dim, kv_heads, page_size, num_pages, ps * D, D, kv_heads * ps * D, 1, box, "V pages", &h->tm_v);
+        if (rc != SEGKV_OK) {
+            free_all(h);
+            delete h;
+            return rc;
+        }
+    }
     *out = h;
     return SEGKV_OK;
 }
@@ -137,6 +166,23 @@ int segkv_pages_sdpa(segkv_pages_t h, int n, int q_len, const void* q, long long
     if (rc != SEGKV_OK || n == 0 || q_len == 0) return rc;
     if (!rows_ok(q, q_stride, (long long)h->heads * h->head_dim) || !out || !aligned(out, 16) || !aligned(alibi_slopes, 4)) return SEGKV_EINVAL;
     if ((long long)n * q_len * h->group > 0x7FFFFFFFLL) return SEGKV_EINVAL;
+    const int pack = pack_log(h, alibi_slopes != nullptr);
+    if (many_rows(h, n, q_len, pack)) {
+        Dims d = {};
+        d.batch = n; d.heads = h->heads >> pack; d.kv_heads = h->kv_heads; d.group = h->group >> pack; d.head_dim = h->head_dim; d.dtype = h->dtype;
+        CUtensorMap tm_q;
+        const long long D = h->head_dim;
+        const int rc2 = encode_map(q, h->dtype == SEGKV_BF16, h->head_dim, h->heads, q_len, n, D, q_stride, q_stride * q_len, 1 << pack, 128 >> pack, "query", &tm_q);
+        if (rc2 != SEGKV_OK) return rc2;
+        PrefillArgs a;
+        a.q = q; a.out = out; a.slopes = alibi_slopes; a.err_word = h->err_word;
+        a.prompt_len = q_len << pack;
+        a.tm_k = &h->tm_k; a.tm_v = &h->tm_v; a.plens = nullptr; a.tm_k_src = a.tm_v_src = nullptr; a.tm_q = &tm_q;
+        a.row_groups = 0; a.pdl = h->overlap; a.wait_ns = 0; a.dbg_skip = false;
+        a.table = table; a.lens = lens; a.table_stride = table_stride; a.page_log = h->page_log; a.num_pages = h->num_pages;
+        a.q_len = q_len; a.pack_log = pack; a.box_log = h->box_log;
+        return launched(h, launch_prefill_tc5(d, a, (cudaStream_t)stream), "segkv_pages_sdpa", stream);
+    }
     PageSdpaArgs a = {n, q_len, q, q_stride, out, table, table_stride, lens, alibi_slopes, h->overlap};
     return launched(h, launch_pages_sdpa(*h, a, (cudaStream_t)stream), "segkv_pages_sdpa", stream);
 }

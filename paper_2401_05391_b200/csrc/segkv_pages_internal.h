@@ -16,6 +16,8 @@ struct segkv_pages {
     float* ws;           // partial results of work groups that several CTAs share: two slots per CTA
     int* tickets;        // [CTAs] arrival counters, zero between launches
     int* err_word;
+    CUtensorMap tm_k, tm_v;   // 16 bits: of the pages, in pieces of box_log rows (as a power of two)
+    int box_log;
 };
 
 namespace segkv_impl {

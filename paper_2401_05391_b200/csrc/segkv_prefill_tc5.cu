@@ -50,6 +50,7 @@
 #include <type_traits>
 
 #include "segkv_internal.h"
+#include "segkv_pages.h"
 #include "segkv_ptx.cuh"
 #include "segkv_tc5.cuh"
 
@@ -72,6 +73,11 @@ struct Tc5Params {
     int paired, rounds;      // item order: see round_item; rounds = items a CTA walks through (some may be empty)
     float scale2;
     uint32_t idesc_qk, idesc_pv;
+    // pages (MODE 3): N is the packed query rows of one (sequence, kv head group), H and G count groups of packed heads
+    const int32_t *table, *lens;
+    int table_stride, page_log, num_pages, q_len;
+    int pack_log;            // query heads of a kv head side by side in the rows, as a power of two
+    int box_log;             // rows of a page that one copy brings, as a power of two
     int dbg_skip;            // test aid: one softmax thread leaves out one barrier arrival, so that a wait runs out
     unsigned long long wait_ns;   // limit of every bounded wait
 };
@@ -142,7 +148,7 @@ constexpr float kSplitSlope = 0.0625f;   // weights fall by e^-slope per key: be
 constexpr int kSplitWindow = 64;
 // Do the `nkeys` keys from `key0` on get two-part weights, for the group whose first row is row0?
 __device__ __forceinline__ bool split_p_keys(int row0, int key0, int nkeys, bool steep) {
-    if (row0 == 0 && key0 < kRows) return true;
+    if (row0 <= 0 && key0 < kRows) return true;
     return steep && key0 + nkeys - 1 >= row0 - kSplitWindow;
 }
 
@@ -210,14 +216,22 @@ __device__ __forceinline__ uint64_t weigh16(const uint32_t* sr, float scale2, fl
 // softmax threads are still storing the previous output.
 // MODE 0: K/V from the prompt segment, one prompt length; 1: fused prefill (K/V from the caller's arrays,
 // every tile stored into the segment); 2: per-request prompt lengths (kept out of the other two: the
-// lengths as run-time values cost registers that the softmax threads of the two-group shape do not have).
+// lengths as run-time values cost registers that the softmax threads of the two-group shape do not have); 3: the newest
+// q_len tokens of sequences whose keys and values lie in pages (segkv_pages_sdpa).  There
+//   * a row is a (token, query head) pair: as many heads of a kv head as are a power of two stand side by side, so that a few tokens
+//     of grouped heads fill a group's 128 rows and K and V are read once for all of them; row r sees the keys up to
+//     lens[b] - q_len + r / heads;
+//   * a K or V tile is copied page by page (pieces of at least 16 rows, all of one (page, kv head)) through a map of the pool in
+//     coordinates (d, kv head, row, page); what lies wholly behind the sequence is asked for behind the page's last row, which
+//     gives zeros, and the rows of the last page that do not exist, whatever they hold, are zeroed in the V tile by the MMA
+//     warp (a weight of 0 times a NaN is a NaN; their scores are masked).
 template <typename T, typename L, int MODE>
 __global__ void __launch_bounds__(L::kThreads, 1)
 prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_k_seg,
                    const __grid_constant__ CUtensorMap tm_v_seg, const Tc5Params p) {
     constexpr int NG = L::NG, NB = L::NB, TPR = L::TPR, SK = L::kStagesK, SV = L::kStagesV;
-    constexpr bool STORE = MODE == 1, RAGGED = MODE == 2;
+    constexpr bool STORE = MODE == 1, RAGGED = MODE == 2, PAGED = MODE == 3;
     constexpr bool kSplitP = sizeof(typename SplitP<T>::yes) != 0 && SplitP<T>::value;
     constexpr int kD = L::D, kKeys = L::KEYS, kTileKV = L::kTileKV, kColTile = L::kColTile;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -270,9 +284,26 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     // nb = the request's own prompt length: with ragged prompts the items are still laid out for the
     // longest one, and a shorter request leaves its later items (and the tail of one) without work.  (Lengths and slopes are read
     // by plain loads: the kernel before may write them, and a read-only load need not stay behind the wait for it below.)
-    auto request_len = [&](int b) -> int { return RAGGED ? p.plens[b] : p.N; };
+    auto request_len = [&](int b) -> int {
+        if constexpr (PAGED) return min(max(p.lens[b], 0), (int)min((long long)p.table_stride << p.page_log, 0x7FFFFFFFLL));
+        return RAGGED ? p.plens[b] : p.N;
+    };
+    // the position of packed row r of a sequence of nb tokens (PAGED; below 0: it sees nothing); rows behind the last see what it sees
+    auto row_pos = [&](int r, int nb) -> int { return min(nb - p.q_len + (r >> p.pack_log), nb - 1); };
+    // what the rule of two-part weights takes for a group's first row: pages, 0 also for any row that sees 128 keys at most
+    auto split_row = [&](int row0, int nb) -> int {
+        if constexpr (PAGED) {
+            const int pos = row_pos(row0, nb);
+            return pos < kRows ? 0 : pos;
+        }
+        return row0;
+    };
     auto group_tiles = [&](int qt, int g, int nb) -> int {
         const int base = (qt * NG + g) * kRows;
+        if constexpr (PAGED) {
+            const int last = base < p.N ? row_pos(min(base + kRows, p.N) - 1, nb) : -1;
+            return last < 0 ? 0 : last / kKeys + 1;
+        }
         return base < nb ? min((nb + kKeys - 1) / kKeys, (base + kRows - 1) / kKeys + 1) : 0;
     };
 
@@ -329,6 +360,20 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                         tma_load_4d(dst + cb * kColTile + rb * L::kBoxBytes, tm, cb * 64, kvh,
                                     kt * kKeys + rb * L::kBoxRows, b, full);
             };
+            // a tile from the pages `ids` (one for each piece; -1: behind the sequence's end)
+            constexpr int kMaxPieces = kKeys / 16;
+            auto load_pages = [&](const CUtensorMap* tm, uint8_t* dst_tile, int kt, int kvh, const int* ids, uint32_t full) {
+                const uint32_t dst = smem_u32(dst_tile);
+                mbar_arrive_expect_tx(full, (uint32_t)kTileKV);
+#pragma unroll
+                for (int rb = 0; rb < kMaxPieces; ++rb) {
+                    if (rb >= kKeys >> p.box_log) break;
+                    const int row = ids[rb] < 0 ? 1 << p.page_log : (kt * kKeys + (rb << p.box_log)) & ((1 << p.page_log) - 1);
+#pragma unroll
+                    for (int cb = 0; cb < L::kDBoxes; ++cb)
+                        tma_load_4d(dst + cb * kColTile + ((rb << p.box_log) * 128), tm, cb * 64, kvh, row, max(ids[rb], 0), full);
+                }
+            };
             uint32_t tp = 0, tk = 0;                               // K/V tiles requested so far (ring position); K tiles alone
             uint32_t qi[NG];                                      // items group g has taken part in: Q barrier phases
 #pragma unroll
@@ -339,6 +384,7 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 if (w >= n_items) continue;
                 const int qt = item_qt(w), hb = w % hb_count, h = hb % p.H, b = hb / p.H;
                 const int kvh = h / p.G;
+                if (PAGED && (unsigned)p.lens[b] != (unsigned)request_len(b)) atomicOr(p.err_word, SEGKV_DEV_BAD_PAGE);
                 int nkt = 0;
 #pragma unroll
                 for (int g = 0; g < NG; ++g) nkt = max(nkt, group_tiles(qt, g, request_len(b)));
@@ -355,18 +401,35 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     mbar_arrive_expect_tx(qfull, (uint32_t)L::kQGroup);
 #pragma unroll
                     for (int cb = 0; cb < L::kDBoxes; ++cb)
-                        tma_load_4d(dst + cb * kBoxQ, &tm_q, cb * 64, h, (qt * NG + g) * kRows, b, qfull);
+                        tma_load_4d(dst + cb * kBoxQ, &tm_q, cb * 64, PAGED ? h << p.pack_log : h,
+                                    PAGED ? ((qt * NG + g) * kRows) >> p.pack_log : (qt * NG + g) * kRows, b, qfull);
                 }
                 for (int i = 0; i < nkt && ok; ++i, ++tp) {
                     const int kt = tile_at(i, nkt);
                     const uint32_t sk = tp % SK, sv = tp % SV;
+                    int ids[kMaxPieces];
+                    if constexpr (PAGED) {
+                        const int len = request_len(b);
+#pragma unroll
+                        for (int rb = 0; rb < kMaxPieces; ++rb) {
+                            const int key = kt * kKeys + (rb << p.box_log);
+                            ids[rb] = -1;
+                            if (rb < kKeys >> p.box_log && key < len) ids[rb] = p.table[(long long)b * p.table_stride + (key >> p.page_log)];
+                            if (rb < kKeys >> p.box_log && key < len && (unsigned)ids[rb] >= (unsigned)p.num_pages) {
+                                atomicOr(p.err_word, SEGKV_DEV_BAD_PAGE);
+                                ids[rb] = 0;
+                            }
+                        }
+                    }
                     ok = mbar_wait(kempty0 + 8 * sk, ((tp / SK) & 1) ^ 1, p.wait_ns);
                     if (!ok) break;
-                    load_tile(&tm_k, k_ring + (size_t)sk * kTileKV, kt, kvh, b, kfull0 + 8 * sk);
+                    if constexpr (PAGED) load_pages(&tm_k, k_ring + (size_t)sk * kTileKV, kt, kvh, ids, kfull0 + 8 * sk);
+                    else load_tile(&tm_k, k_ring + (size_t)sk * kTileKV, kt, kvh, b, kfull0 + 8 * sk);
                     tk = tp + 1;
                     ok = mbar_wait(vempty0 + 8 * sv, ((tp / SV) & 1) ^ 1, p.wait_ns);
                     if (!ok) break;
-                    load_tile(&tm_v, v_ring + (size_t)sv * kTileKV, kt, kvh, b, vfull0 + 8 * sv);
+                    if constexpr (PAGED) load_pages(&tm_v, v_ring + (size_t)sv * kTileKV, kt, kvh, ids, vfull0 + 8 * sv);
+                    else load_tile(&tm_v, v_ring + (size_t)sv * kTileKV, kt, kvh, b, vfull0 + 8 * sv);
                 }
             }
             if (!ok) s_abort = 1;
@@ -468,7 +531,7 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             for (int j = 0; j < p.rounds && ok; ++j) {
                 const int w = round_item(j);
                 if (w >= n_items) continue;
-                const int qt = item_qt(w), nb = RAGGED ? (int)__reduce_max_sync(0xffffffffu, (unsigned)request_len((w % hb_count) / p.H)) : p.N;
+                const int qt = item_qt(w), nb = RAGGED || PAGED ? (int)__reduce_max_sync(0xffffffffu, (unsigned)request_len((w % hb_count) / p.H)) : p.N;
                 // is the head's slope one of those whose weights go in two parts next to the diagonal?
                 const bool steep = kSplitP && p.slopes && __any_sync(0xffffffffu, p.slopes[(w % hb_count) % p.H] >= kSplitSlope);
                 int gt[NG], nkt = 0;
@@ -513,6 +576,15 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     const uint64_t vd = dv + (v_lo0 + vst * (uint32_t)(kTileKV >> 4));
                     ok = wait(vfull0 + 8 * vst, vph);
                     if (!ok) break;
+                    if (PAGED && (kt + 1) * kKeys > nb) {         // rows of the last page that do not exist
+                        const int v0 = nb - kt * kKeys, v1 = ((v0 + (1 << p.box_log) - 1) >> p.box_log) << p.box_log;
+                        uint8_t* tile = v_ring + (size_t)vst * kTileKV;
+                        for (int i = v0 * 8 + lane; i < v1 * 8; i += 32)
+#pragma unroll
+                            for (int cb = 0; cb < L::kDBoxes; ++cb) *reinterpret_cast<uint4*>(tile + cb * kColTile + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        fence_proxy_async();
+                        __syncwarp();
+                    }
                     bool k_next = false;
 #pragma unroll
                     for (int g = 0; g < NG; ++g) {
@@ -526,10 +598,10 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                             for (int kk = 0; kk < kKeys / 16; ++kk)   // O_g += P_g[:, 16 keys] . V[16 keys, :]
                                 tc_mma_ts_if(lead, tmem + (uint32_t)(L::kColO + kD * g), p_tmem + kk * 16,
                                              vd + (uint64_t)((kk * 2048) >> 4), p.idesc_pv, (i != first[g] || kk > 0));
-                            if (kSplitP && split_p_keys((qt * NG + g) * kRows, kt * kKeys, kKeys, steep)) {
+                            if (kSplitP && split_p_keys(split_row((qt * NG + g) * kRows, nb), kt * kKeys, kKeys, steep)) {
 #pragma unroll
                                 for (int kk = 0; kk < kKeys / 16; ++kk)   // ... and the low parts of the weights that have one
-                                    if (split_p_keys((qt * NG + g) * kRows, kt * kKeys + 16 * kk, 16, steep))
+                                    if (split_p_keys(split_row((qt * NG + g) * kRows, nb), kt * kKeys + 16 * kk, 16, steep))
                                         tc_mma_ts_if(lead, tmem + (uint32_t)(L::kColO + kD * g), p_tmem + kk * 16 + 8,
                                                      vd + (uint64_t)((kk * 2048) >> 4), p.idesc_pv, 1u);
                             }
@@ -572,13 +644,31 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const size_t qstride = (size_t)p.H * kD;
         uint32_t n = 0;                                           // tiles of this group so far: barrier phases
         bool ok = true, gone = false;                             // a wait of this thread ran out; the row's warps have agreed to leave
+        // element of packed row `row` of (sequence b, head group h) in the output
+        auto packed_at = [&](int b, int h, int row) -> size_t {
+            return (((size_t)b * p.q_len + (row >> p.pack_log)) * ((size_t)p.H << p.pack_log) + ((size_t)h << p.pack_log) + (row & ((1 << p.pack_log) - 1))) * kD;
+        };
         for (int j = 0; j < p.rounds && !gone; ++j) {
             const int w = round_item(j);
             if (w >= n_items) continue;
             const int qt = item_qt(w), hb = w % hb_count, h = hb % p.H, b = hb / p.H;
             const int my_tiles = group_tiles(qt, g, request_len(b));
-            if (my_tiles == 0) continue;
-            const int row0 = (qt * NG + g) * kRows, row = row0 + r;
+            const int prow0 = (qt * NG + g) * kRows;              // first packed row of the group
+            if (my_tiles == 0) {
+                // (pages: rows of tokens before the sequence's start, which see nothing, are zeros)
+                if (PAGED && prow0 + r < p.N) {
+                    uint4* o = reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.out) + packed_at(b, h, prow0 + r) + DH * part);
+#pragma unroll 1
+                    for (int i = 0; i < DH / 8; ++i) o[i] = make_uint4(0u, 0u, 0u, 0u);
+                }
+                continue;
+            }
+            const int nb = request_len(b);
+            // positions: of the group's first row, of this thread's, and of the first and the last of the warp
+            const int row = PAGED ? row_pos(prow0 + r, nb) : prow0 + r;
+            const int wfirst = PAGED ? row_pos(prow0 + (warp & 3) * 32, nb) : prow0 + (warp & 3) * 32;
+            const int wlast = PAGED ? row_pos(prow0 + (warp & 3) * 32 + 31, nb) : prow0 + (warp & 3) * 32 + 31;
+            const int srow0 = split_row(prow0, nb);
             const float slope_nat = p.slopes ? p.slopes[h] : 0.f;
             const float slope2 = slope_nat * 1.4426950408889634f;
             const bool biased = back;
@@ -595,7 +685,7 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 const int key0 = kt * kKeys + part * KH;
                 const int lim = row - key0;                        // key index i is visible iff i <= lim
                 const float bias0 = slope2 * (float)(key0 - row);
-                const bool two = kSplitP && split_p_keys(row0, kt * kKeys, kKeys, slope_nat >= kSplitSlope);
+                const bool two = kSplitP && split_p_keys(srow0, kt * kKeys, kKeys, slope_nat >= kSplitSlope);
                 float alpha = 1.f;
                 uint64_t ls = 0ull;
                 int kept = 0;                                     // keys whose weights are stored
@@ -605,9 +695,9 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 // two scores, on the chain that sets the pace.  Not where no key has been visible to a
                 // row so far, nor under a negative slope, whose maximum grows from tile to tile towards the oldest key: there the
                 // reference follows it exactly, so that the weight of the key that counts most is not rounded.)
-                const bool fresh = t == 0 || slope2 < 0.f || __any_sync(0xffffffffu, m_ref == -INFINITY);
-                const int seen = row0 + (warp & 3) * 32 + 32 - key0;       // keys that some row of the warp sees
-                const bool mask = key0 + KH - 1 > row0 + (warp & 3) * 32;  // keys that some row of the warp does not see
+                const bool fresh = t == 0 || slope2 < 0.f || (PAGED && biased && key0 + KH - 1 > wfirst) || __any_sync(0xffffffffu, m_ref == -INFINITY);
+                const int seen = wlast + 1 - key0;                         // keys that some row of the warp sees
+                const bool mask = key0 + KH - 1 > wfirst;                  // keys that some row of the warp does not see
                 bool stands = false;
                 if (!fresh) {
                     if (ok) {
@@ -803,12 +893,13 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll
             for (int i = 0; i < TPR; ++i) l_run += xrow[i * kRows];
             bar_sync_n(rows_bar, 32 * TPR);
-            const float inv = 1.f / l_run;
+            const float inv = PAGED && l_run == 0.f ? 0.f : 1.f / l_run;
             // NP lanes trade 16-byte pieces of their rows, so that a store instruction writes 64 (32) bytes of each of 8 (16) rows
             // instead of 16 of 32: with one row per lane the stores of an item took 3400 clocks (6500 at head_dim 256).
             constexpr int EC = DH < 32 ? DH : 32, NP = EC / 8;    // columns at a time; pieces of a row and lanes that trade
-            const int len = request_len(b), rowq = row0 + (r & ~(NP - 1));
-            T* oq = reinterpret_cast<T*>(p.out) + ((size_t)b * p.N * p.H + h) * kD + (size_t)rowq * qstride + DH * part + (lane & (NP - 1)) * 8;
+            const int len = PAGED ? p.N : nb, rowq = prow0 + (r & ~(NP - 1));
+            T* oq = reinterpret_cast<T*>(p.out) + DH * part + (lane & (NP - 1)) * 8;
+            if (!PAGED) oq += ((size_t)b * p.N * p.H + h) * kD + (size_t)rowq * qstride;
 #pragma unroll 1
             for (int c = 0; c < DH / EC; ++c) {
                 uint32_t orr[EC];
@@ -839,7 +930,7 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll
                 for (int i = 0; i < NP; ++i)
                     if (rowq + i < len)
-                        *reinterpret_cast<uint4*>(oq + (size_t)i * qstride + c * EC) = make_uint4(v[i][0], v[i][1], v[i][2], v[i][3]);
+                        *reinterpret_cast<uint4*>(oq + (PAGED ? packed_at(b, h, rowq + i) : (size_t)i * qstride) + c * EC) = make_uint4(v[i][0], v[i][1], v[i][2], v[i][3]);
             }
         }
         if (!ok && lane == 0) s_abort = 1;
@@ -897,6 +988,8 @@ cudaError_t launch_tc5(const Dims& d, const PrefillArgs& a, Tc5Params p, int sms
             e = cudaFuncSetAttribute(prefill_tc5_kernel<T, L, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e == cudaSuccess)
             e = cudaFuncSetAttribute(prefill_tc5_kernel<T, L, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(prefill_tc5_kernel<T, L, 3>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
         configured[dev] = true;
     }
@@ -914,7 +1007,7 @@ cudaError_t launch_tc5(const Dims& d, const PrefillArgs& a, Tc5Params p, int sms
         const int nqt = (a.prompt_len + kRows * NG - 1) / (kRows * NG), ppb = (nqt + 1) / 2;
         const long hb_count = (long)d.heads * d.batch;
         const int bpw = ppb <= sms ? sms / ppb : 0;
-        p.paired = (grid == (unsigned)sms && bpw > 0 && hb_count >= 4L * bpw && deal_in_pairs(d, a.prompt_len, p.slopes != nullptr, nqt, bpw, sms)) ? 1 : 0;
+        p.paired = (!p.table && grid == (unsigned)sms && bpw > 0 && hb_count >= 4L * bpw && deal_in_pairs(d, a.prompt_len, p.slopes != nullptr, nqt, bpw, sms)) ? 1 : 0;
         p.rounds = p.paired ? 2 * (int)((hb_count + bpw - 1) / bpw) : (int)((items + grid - 1) / grid);
     }
     // fused prefill: load through the maps over the caller's arrays, store through the segment's
@@ -929,6 +1022,7 @@ cudaError_t launch_tc5(const Dims& d, const PrefillArgs& a, Tc5Params p, int sms
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = a.pdl ? 1 : 0;
+    if (p.table) return cudaLaunchKernelEx(&cfg, prefill_tc5_kernel<T, L, 3>, *a.tm_q, *a.tm_k, *a.tm_v, *a.tm_k, *a.tm_v, p);
     if (store) return cudaLaunchKernelEx(&cfg, prefill_tc5_kernel<T, L, 1>, *a.tm_q, *a.tm_k_src, *a.tm_v_src, *a.tm_k, *a.tm_v, p);
     if (p.plens) return cudaLaunchKernelEx(&cfg, prefill_tc5_kernel<T, L, 2>, *a.tm_q, *a.tm_k, *a.tm_v, *a.tm_k, *a.tm_v, p);
     return cudaLaunchKernelEx(&cfg, prefill_tc5_kernel<T, L, 0>, *a.tm_q, *a.tm_k, *a.tm_v, *a.tm_k, *a.tm_v, p);
@@ -963,6 +1057,8 @@ cudaError_t launch_prefill_tc5(const Dims& d, const PrefillArgs& a, cudaStream_t
     p.plens = a.plens;
     p.N = a.prompt_len; p.H = d.heads; p.G = d.group; p.B = d.batch;
     p.scale2 = 0.f; p.idesc_qk = p.idesc_pv = 0; p.snake = 0; p.paired = 0; p.rounds = 0;
+    p.table = a.table; p.lens = a.lens; p.table_stride = a.table_stride; p.page_log = a.page_log; p.num_pages = a.num_pages;
+    p.q_len = a.q_len; p.pack_log = a.pack_log; p.box_log = a.box_log;
     p.dbg_skip = a.dbg_skip ? 1 : 0;
     p.wait_ns = a.wait_ns ? a.wait_ns : kWaitLimitNs;
     int sms = 148;

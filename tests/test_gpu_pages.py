@@ -83,6 +83,41 @@ def test_attention(shape, dtype, bits):
     c.destroy()
 
 
+MANY = [
+    # heads, kv_heads, D, page, q_len, lens: pieces of prompts, on the fifth-generation tensor cores where they fill them
+    (1, 1, 64, 16, 128, [128]),
+    (4, 4, 64, 16, 200, [200, 333, 150, 0, 1]),
+    (32, 4, 128, 64, 64, [64, 65, 700, 63, 1]),
+    (8, 8, 128, 16, 129, [129, 130, 256, 257, 100]),
+    (12, 4, 128, 256, 150, [400, 151]),
+    (16, 1, 128, 32, 300, [1000, 77]),
+    (32, 1, 64, 128, 33, [33, 500]),
+    (8, 2, 256, 16, 140, [140, 300, 17]),
+    (2, 2, 256, 128, 257, [600]),
+    (16, 16, 64, 32, 250, [250 + 7 * i for i in range(20)]),          # two groups of rows per CTA
+    (8, 8, 128, 16, 256, [256 + 61 * (i % 5) for i in range(38)]),
+]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("shape", MANY, ids=lambda s: "x".join(map(str, s[:5])))
+def test_attention_of_many_rows(shape, dtype):
+    H, Hkv, D, ps, T, lens = shape
+    seed = 7 * H + D + ps + T
+    c, table, n_lens = filled(H, Hkv, D, ps, lens, dtype, 16, seed, poison=True)
+    for alibi in (False, True):
+        x = randn(len(lens), T, H + 2, D, dtype=dtype, g=gen(seed + 1))
+        q = x[:, :, 1:H + 1] if D == 64 else x[:, :, :H].contiguous()
+        slopes = wl.alibi_slopes(H).cuda() if alibi else None
+        out = torch.full((len(lens), T, H, D), math.nan, dtype=dtype, device="cuda")
+        c.sdpa(q, table, n_lens, out, slopes)
+        pg.check(out, *pg.attention(c, q, table, lens, slopes))
+        again = c.sdpa(q, table, n_lens, None, slopes)
+        assert torch.equal(out, again)
+    assert c.get_error() == 0
+    c.destroy()
+
+
 @pytest.mark.parametrize("bits,dtype,H,Hkv,D,T,lens", [
     (16, F16, 4, 1, 128, 1, [20011]), (4, F16, 4, 1, 128, 1, [20011]), (16, BF16, 16, 2, 64, 1, [9999, 3, 70]),
     (4, BF16, 16, 2, 256, 1, [5000, 12000]), (4, F16, 9, 1, 64, 2, [30001]), (16, F16, 2, 2, 256, 1, [7777]),
