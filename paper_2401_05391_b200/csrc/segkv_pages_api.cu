@@ -1,5 +1,4 @@
 // Host side of the paged cache: handle life cycle, argument checks, launches.
-#include <stdlib.h>
 #include <string.h>
 
 #include <new>
@@ -52,11 +51,19 @@ int pack_log(const segkv_pages* h, bool slopes) {
     return g;
 }
 
-// Does the tensor-core kernel serve the call?
+// Does the kernel on the fifth-generation tensor cores serve the call?  It takes 128 rows (tokens times packed heads) of a kv head on a
+// CTA of its own, and a round of one such item per SM takes r for 128 keys, however many of the rows are real; the warp-level kernel takes
+// u for 128 keys of every tile of 16 columns (8 at head_dim 256), spread over all SMs.  Both go with the keys' number, which only the device
+// knows, so that the ratio decides.  Measured (2560 keys, us, warp-level / tensor cores): head_dim 128, 32 x 4 heads, 2 sequences of 16
+// tokens 20.4 / 31.8, of 64 37.9 / 32.1, of 128 64.0 / 32.2, of 512 207 / 61.8, 16 of 5 39.5 / 33.3, 64 of 4 111 / 64.2; one of 64 at 32768 keys 168 /
+// 346; 32 x 32 heads, 4 of 32 45.6 / 34.1; head_dim 256, 16 x 16, 4 of 64 193 / 52.9; head_dim 64, 32 x 8, 4 of 64 43.9 / 31.6.
 bool many_rows(const segkv_pages* h, int n, int q_len, int pack) {
     if (h->bits != 16) return false;
-    static const char* x = getenv("SEGKV_X");
-    return x ? atoi(x) != 0 : (long long)q_len << pack >= 128;
+    const long long cols = (long long)q_len * h->group, nc = h->head_dim == 256 ? 8 : 16, ctiles = (cols + nc - 1) / nc;
+    if (ctiles < 2) return false;
+    const long long items = (long long)n * (h->heads >> pack) * ((((long long)q_len << pack) + 127) / 128);
+    const double u = h->head_dim == 64 ? 4.3 : h->head_dim == 128 ? 7.0 : 18.8, r = h->head_dim == 256 ? 2600.0 : 1550.0;      // ns
+    return (double)n * h->kv_heads * ctiles * u > (double)((items + h->sm_count - 1) / h->sm_count) * r;
 }
 
 void free_all(segkv_pages* h) {
