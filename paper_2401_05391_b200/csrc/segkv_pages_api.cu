@@ -1,5 +1,4 @@
 // Host side of the paged cache: handle life cycle, argument checks, launches.
-#include <stdlib.h>
 #include <string.h>
 
 #include <new>
@@ -192,8 +191,6 @@ int segkv_pages_sdpa(segkv_pages_t h, int n, int q_len, const void* q, long long
         return launched(h, launch_prefill_tc5(d, a, (cudaStream_t)stream), "segkv_pages_sdpa", stream);
     }
     PageSdpaArgs a = {n, q_len, q, q_stride, out, table, table_stride, lens, alibi_slopes, h->overlap};
-    static const char* xx = getenv("SEGKV_X");
-    if (h->bits == 4 && (!xx || atoi(xx))) return launched(h, launch_pages_tc5(*h, a, (cudaStream_t)stream), "segkv_pages_sdpa", stream);
     return launched(h, launch_pages_sdpa(*h, a, (cudaStream_t)stream), "segkv_pages_sdpa", stream);
 }
 

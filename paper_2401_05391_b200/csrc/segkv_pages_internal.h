@@ -56,7 +56,6 @@ struct PageSdpaArgs {
 
 cudaError_t launch_pages_append(const segkv_pages& h, const PageAppendArgs& a, cudaStream_t st);
 cudaError_t launch_pages_read(const segkv_pages& h, const PageTokens& t, void* k_out, void* v_out, cudaStream_t st);
-cudaError_t launch_pages_tc5(const segkv_pages& h, const PageSdpaArgs& a, cudaStream_t st);      // 4-bit pages, for work that fills the GPU
 cudaError_t launch_pages_sdpa(const segkv_pages& h, const PageSdpaArgs& a, cudaStream_t st);
 int pages_sdpa_grid(const segkv_pages& h);                  // most CTAs of an attention launch
 size_t pages_sdpa_slot_floats(const segkv_pages& h);        // floats of one CTA's partial result

@@ -13,14 +13,32 @@
 // side by side, so a 16-key tile is one contiguous piece.
 #include <atomic>
 
-#include "segkv_pages_sdpa.cuh"
+#include "segkv_pages_internal.h"
+#include "segkv_ptx.cuh"
 
 namespace segkv_impl {
 namespace {
 
-using namespace pages;
+using namespace ptx;
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr float kLog2e = 1.4426950408889634f;
+// A column's weights are taken relative to a reference that is only moved when a score exceeds it by 2^kSlack.
+constexpr float kSlack = 8.f;
+
+struct Params {
+    const char* q;
+    long long q_stride;              // bytes
+    char* out;
+    const char *kp, *vp;
+    const int32_t *table, *lens;
+    const float* slopes;
+    float* ws;
+    int* tickets;
+    int* err;
+    int table_stride, n, q_len, H, Hkv, group, page_log, num_pages;
+    int cols, ctiles;                // query columns of a (sequence, kv head), tiles of them
+};
 
 template <typename T> struct Num;
 template <> struct Num<__half> {
@@ -40,6 +58,30 @@ template <> struct Num<__nv_bfloat16> {
     }
 };
 
+// ---- 4-bit rows: codes as fp16, whatever the dtype ----------------------------------------------------------------------------
+// Two codes of a word, in bits 0-3 and 16-19, become fp16 numbers by or-ing them into 1024 (whose last place is 1); codes in bits 4-7 and
+// 20-23 count 16.  An fp16 product takes them exactly, so the queries (scaled by a power of two per column) and the weights are
+// fp16 for a bf16 cache too: 11 bits instead of 8, and half the shifts.
+constexpr uint32_t kMagic = 0x64006400u;
+constexpr float kLift4 = 6.f;
+// (w & mask) | magic in one instruction
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(kMagic));
+    return r;
+}
+__device__ __forceinline__ uint32_t codes_lo(uint32_t w) { return and_or(w, 0x000F000Fu); }          // 1024 + c
+__device__ __forceinline__ uint32_t codes_hi(uint32_t w) { return and_or(w, 0x00F000F0u); }          // 1024 + 16 c
+__device__ __forceinline__ uint32_t centred_lo(uint32_t w) {                                         // c - 8
+    const uint32_t x = codes_lo(w), k = 0x64086408u;                                                 // 1032
+    const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&k));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t centred_hi(uint32_t w) {                                         // (1024 + 16 c) / 16 - 72
+    const uint32_t x = codes_hi(w), m = 0x2C002C00u, k = 0xD480D480u;
+    const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&m), *reinterpret_cast<const __half2*>(&k));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
 __device__ __forceinline__ void mma_h(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1, float c2, float c3) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
@@ -93,7 +135,7 @@ template <int D, int NT, int BITS> struct Shape {
     static constexpr int SMEM = RING + MERGE + ML + 64;
     static constexpr int CTAS = ctas_per_sm(D, NC, BITS);
     static constexpr int MT = D / 16;                                         // 16-channel tiles of the output
-    static constexpr int SLOT = kSlot<D, NC>;
+    static constexpr int SLOT = NC * (D + 2);
 };
 
 // Where 16-byte chunk c of row k (0..15) of a 16-row piece lies: 4-bit rows, whose readers take a row's bytes by fours of lanes and
@@ -102,6 +144,42 @@ template <int D> __device__ __forceinline__ uint32_t code_at(int k, int c) {
     if (D == 64) return (k >> 2) * 128 + ((((k & 3) * 2 + c) ^ (((k >> 2) & 1) * 4)) * 16);
     if (D == 128) return (k >> 1) * 128 + ((((k & 1) * 4 + c) ^ ((((k >> 1) & 1) << 1) | (((k >> 2) & 1) << 2))) * 16);
     return k * 128 + ((c ^ (((k & 3) << 1) ^ (((k >> 2) & 1) << 2))) * 16);
+}
+
+struct Cursor {                      // a block of keys in the grid's order
+    int v, h, b, nb, klen;
+    const int32_t* row;              // the sequence's pages
+};
+
+// Keys that column tile ct of sequence s reads, and how many blocks that makes (at least one: an empty sequence's output is written too).
+template <int NC, int KB>
+__device__ __forceinline__ void extent(const Params& p, int v, int* klen, int* nb, bool flag) {
+    const int s = v / p.ctiles, ct = v - s * p.ctiles;
+    const int most = (int)min((long long)p.table_stride << p.page_log, 0x7FFFFFFFLL);
+    int len = __ldg(p.lens + s);
+    if (len < 0 || len > most) {
+        if (flag) atomicOr(p.err, SEGKV_DEV_BAD_PAGE);
+        len = len < 0 ? 0 : most;
+    }
+    const int last = min(p.cols, (ct + 1) * NC) - 1;
+    int k = len - p.q_len + last / p.group + 1;
+    k = k < 0 ? 0 : k;
+    *klen = k;
+    *nb = k > KB ? (k + KB - 1) / KB : 1;
+}
+
+template <int NC, int KB>
+__device__ __forceinline__ void enter(const Params& p, Cursor& c) {
+    extent<NC, KB>(p, c.v, &c.klen, &c.nb, false);
+    c.row = p.table + (long long)(c.v / p.ctiles) * p.table_stride;
+}
+template <int NC, int KB>
+__device__ __forceinline__ void advance(const Params& p, Cursor& c, int V) {
+    if (++c.b < c.nb) return;
+    c.b = 0;
+    if (++c.h < p.Hkv) return;
+    c.h = 0;
+    if (++c.v < V) enter<NC, KB>(p, c);
 }
 
 template <typename T, int D, int NT, int BITS>
@@ -122,11 +200,64 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    Run run;
-    if (!find_run<NC, KB, kWarps>(p, reinterpret_cast<long long*>(s_merge), s_misc, run)) return;      // (every thread)
-    const int V = run.V, G = run.G, cta = blockIdx.x, blocks = run.blocks;
-    const unsigned long long total = run.total;
-    Cursor ld = run.first, cur = run.first;
+    // ---- this CTA's run of blocks -------------------------------------------------------------------------------------------
+    const int V = p.n * p.ctiles;
+    const int per = (V + kThreads - 1) / kThreads;
+    int G = gridDim.x;
+    const int cta = blockIdx.x;
+    unsigned long long x0, x1, total;
+    Cursor ld;
+    {
+        long long* s_scan = reinterpret_cast<long long*>(s_merge);
+        long long mine = 0;
+        const int v0 = min(tid * per, V), v1 = min(v0 + per, V);
+        int klen, nb;
+        for (int v = v0; v < v1; ++v) {
+            extent<NC, KB>(p, v, &klen, &nb, cta == 0);
+            mine += nb;
+        }
+        long long incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long u = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += u;
+        }
+        if (lane == 31) s_scan[warp] = incl;
+        __syncthreads();
+        long long before = incl - mine, all = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) before += s_scan[w];
+            all += s_scan[w];
+        }
+        total = (unsigned long long)all * p.Hkv;
+        if (total < (unsigned long long)G) G = (int)total;    // every CTA of a shared work group has to have a part
+        if (cta >= G) return;                                 // (every thread)
+        x0 = total * cta / G;
+        x1 = total * (cta + 1) / G;
+        unsigned long long at = (unsigned long long)before * p.Hkv;
+        if (mine > 0 && x0 >= at && x0 < at + (unsigned long long)mine * p.Hkv) {
+            for (int v = v0;; ++v) {
+                extent<NC, KB>(p, v, &klen, &nb, false);
+                const unsigned long long size = (unsigned long long)nb * p.Hkv;
+                if (x0 < at + size) {
+                    const unsigned rest = (unsigned)(x0 - at);
+                    s_misc[0] = v;
+                    s_misc[1] = (int)(rest / (unsigned)nb);
+                    s_misc[2] = (int)(rest % (unsigned)nb);
+                    break;
+                }
+                at += size;
+            }
+        }
+        __syncthreads();
+        ld.v = s_misc[0];
+        ld.h = s_misc[1];
+        ld.b = s_misc[2];
+        enter<NC, KB>(p, ld);
+    }
+    Cursor cur = ld;
+    const int blocks = (int)(x1 - x0);
 
     // ---- copies -------------------------------------------------------------------------------------------------------------
     int pid[SUB];                                             // pages of the next tile to be copied
@@ -221,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
     float zo[BITS == 4 ? NT : 1][4];
     int vexp;                                                 // 4 bits: exponent that the values' scales are taken relative to
 
-    unsigned long long x = run.x0;
+    unsigned long long x = x0;
     for (int done = 0; done < blocks;) {
         // ---- a work group, or this CTA's part of it ----------------------------------------------------------------------------
         const int s = cur.v / p.ctiles, ct = cur.v - s * p.ctiles;
@@ -691,7 +822,66 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
             __syncthreads();
             if (s_misc[3] == c1 - c0) {
                 if (tid == 0) p.tickets[c0] = 0;              // as the next launch expects it
-                fold_parts<T, D, NC>(p, s, ct, cur.h, c0, c1, tid);
+                const int parts = c1 - c0 + 1;
+                constexpr int AT = D == 256 ? 4 : 8;          // parts whose loads are in flight together
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const int lcol = nt * 8 + mcol, col = ct * NC + lcol;
+                    float top = -INFINITY, sum = 0.f;
+                    float4 acc[D / 64];
+#pragma unroll
+                    for (int r = 0; r < D / 64; ++r) acc[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int i0 = 0; i0 < parts; i0 += AT) {
+                        float m[AT], l[AT];
+                        float4 v[AT][D / 64];
+#pragma unroll
+                        for (int i = 0; i < AT; ++i) {
+                            m[i] = -INFINITY;
+                            l[i] = 0.f;
+#pragma unroll
+                            for (int r = 0; r < D / 64; ++r) v[i][r] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (i0 + i >= parts) continue;
+                            const float* src = p.ws + ((size_t)(c0 + i0 + i) * 2 + (i0 + i == 0 ? 1 : 0)) * Sh::SLOT;
+                            m[i] = __ldcg(src + NC * D + lcol);
+                            l[i] = __ldcg(src + NC * D + NC + lcol);
+#pragma unroll
+                            for (int r = 0; r < D / 64; ++r) v[i][r] = __ldcg(reinterpret_cast<const float4*>(src + lcol * D + 64 * r + mloc));
+                        }
+                        float mx = top;
+#pragma unroll
+                        for (int i = 0; i < AT; ++i) mx = fmaxf(mx, m[i]);
+                        const float keep = top == -INFINITY ? 1.f : exp2f(top - mx);
+                        sum *= keep;
+#pragma unroll
+                        for (int r = 0; r < D / 64; ++r) {
+                            acc[r].x *= keep; acc[r].y *= keep; acc[r].z *= keep; acc[r].w *= keep;
+                        }
+                        top = mx;
+#pragma unroll
+                        for (int i = 0; i < AT; ++i) {
+                            const float fi = m[i] == -INFINITY ? 1.f : exp2f(m[i] - mx);        // (no weight: zeros, or NaN)
+                            sum = fmaf(l[i], fi, sum);
+#pragma unroll
+                            for (int r = 0; r < D / 64; ++r) {
+                                acc[r].x = fmaf(v[i][r].x, fi, acc[r].x);
+                                acc[r].y = fmaf(v[i][r].y, fi, acc[r].y);
+                                acc[r].z = fmaf(v[i][r].z, fi, acc[r].z);
+                                acc[r].w = fmaf(v[i][r].w, fi, acc[r].w);
+                            }
+                        }
+                    }
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                    if (col < p.cols) {
+                        const int row = col / p.group, hq = cur.h * p.group + (col - row * p.group);
+#pragma unroll
+                        for (int r = 0; r < D / 64; ++r) {
+                            uint2 w2;
+                            w2.x = M::pack(acc[r].x * inv, acc[r].y * inv);
+                            w2.y = M::pack(acc[r].z * inv, acc[r].w * inv);
+                            *reinterpret_cast<uint2*>(p.out + ((((size_t)s * p.q_len + row) * p.H + hq) * D + 64 * r + mloc) * 2) = w2;
+                        }
+                    }
+                }
             }
         }
         done += count;
