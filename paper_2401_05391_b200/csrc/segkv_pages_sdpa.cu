@@ -117,18 +117,22 @@ __device__ __forceinline__ void cp16_all(uint32_t dst, const void* src) {
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+// 4 bits, one or two columns (NARROW): the eight columns of a product are the four groups of each.  A lane then has one group's part of a
+// score: it needs that group's scale and zero point only, and the four lanes of a key add up; the weights times the group's scale
+// are what the lane holds anyhow, in one fragment instead of four; of the output each channel's own group counts.
+
 // CTAs on an SM: what shared memory and registers allow.
 constexpr int ctas_per_sm(int D, int nc, int bits) { return bits == 16 ? (D == 256 ? 1 : 2) : D == 256 || nc == 16 ? 2 : 3; }
 constexpr int kStages = 3;
 
 // Shared-memory shape of a variant.  NT: tiles of eight query columns; a warp's tile is SUB pieces of 16 keys.
-template <int D, int NT, int BITS> struct Shape {
+template <int D, int NT, int BITS, bool NARROW> struct Shape {
     static constexpr int SUB = BITS == 16 ? (D == 64 ? 2 : 1) : (D == 256 ? 1 : 2);
     static constexpr int TK = 16 * SUB, KB = kWarps * TK;
     static constexpr int RB = BITS == 16 ? 2 * D : D / 2;                     // bytes of a row without its scales
     static constexpr int VOFF = TK * RB, SOFF = 2 * TK * RB;
     static constexpr int STAGE = 2 * TK * (RB + (BITS == 4 ? 16 : 0));
-    static constexpr int NC = 8 * NT;
+    static constexpr int NC = NARROW ? 2 : 8 * NT;                            // query columns
     static constexpr int RING = kWarps * kStages * STAGE;
     static constexpr int MERGE = kWarps * 8 * 68 * 4;                         // 64 channels of eight columns of every warp
     static constexpr int ML = kWarps * NC * 2 * 4;
@@ -182,9 +186,10 @@ __device__ __forceinline__ void advance(const Params& p, Cursor& c, int V) {
     if (++c.v < V) enter<NC, KB>(p, c);
 }
 
-template <typename T, int D, int NT, int BITS>
-__global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa_kernel(const __grid_constant__ Params p) {
-    using Sh = Shape<D, NT, BITS>;
+template <typename T, int D, int NT, int BITS, bool NARROW, bool BIAS>
+__global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pages_sdpa_kernel(const __grid_constant__ Params p) {
+    using Sh = Shape<D, NT, BITS, NARROW>;
+    static_assert(!NARROW || (NT == 1 && BITS == 4), "two columns of 4-bit rows");
     using M = Mma<T>;
     using N = Num<T>;
     constexpr int NC = Sh::NC, KB = Sh::KB, TK = Sh::TK, SUB = Sh::SUB, MT = Sh::MT, RB = Sh::RB;
@@ -345,6 +350,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
     uint32_t qf[NT][QJ][2];
     float cinit[BITS == 4 ? NT : 1][4][2];                    // 4 bits: what the magic number adds to a group's sum, negated
     uint32_t qsum[BITS == 4 ? NT : 1];                        // 4 bits: the groups' sums of q, in two parts (B operand)
+    float qs[2];                                              // NARROW: this lane's group's sums
     int lim[NT][2];                                           // keys below it are seen
     float scale2[NT][2], slope[NT][2];                        // of a raw score; of a key's distance, in raw scores
     float mref[NT][2], thr[NT][2], base[NT][2], lsum[NT][2];  // reference, what moves it, its exponent; sum of weights
@@ -363,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
         const int pos0 = cur.klen - 1 - last_row;             // position of row 0; below 0 where the sequence is shorter than q_len
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int col = ct * NC + nt * 8 + g;
+            const int col = ct * NC + (NARROW ? g & 1 : nt * 8 + g);
             const bool real = col < p.cols;
             const int row = real ? col / p.group : 0, hq = cur.h * p.group + (real ? col - row * p.group : 0);
             const char* qr = p.q + ((long long)s * p.q_len + row) * p.q_stride + (size_t)hq * (2 * D);
@@ -405,9 +411,11 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {             // group j: channels j and j + 4 of the eight; odd groups' codes count 16
                         const float by = j & 1 ? 0.0625f : 1.f;
-                        qf[nt][j * (W / 2) + (w >> 1)][w & 1] = Mma<__half>::pack(lo[j] * by, hi[j] * by);
-                        const float2 f = Mma<__half>::unpack(qf[nt][j * (W / 2) + (w >> 1)][w & 1]);
+                        uint32_t& qw = qf[nt][j * (W / 2) + (w >> 1)][w & 1];
+                        qw = Mma<__half>::pack(lo[j] * by, hi[j] * by);
+                        const float2 f = Mma<__half>::unpack(qw);
                         sum[j] += f.x + f.y;                  // (of what the product sees, times 16 where it counts 16)
+                        if (NARROW && j != g >> 1) qw = 0u;   // (column g: group g / 2)
                     }
                 }
 #pragma unroll
@@ -415,23 +423,33 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                     sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 1);
                     sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 2);
                     const float off = sum[j] * (j & 1 ? -(1024.f + 128.f) : -1032.f);
+                    if (!NARROW)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) cinit[nt][j][e] = __shfl_sync(0xffffffffu, off, (2 * t + e) * 4);
+                        for (int e = 0; e < 2; ++e) cinit[nt][j][e] = __shfl_sync(0xffffffffu, off, (2 * t + e) * 4);
                     if (j & 1) sum[j] *= 16.f;
                 }
-                const float a = t & 1 ? sum[2] : sum[0], b = t & 1 ? sum[3] : sum[1];
-                const uint32_t hi = M::pack(a, b);
-                const float2 hf = M::unpack(hi);
-                qsum[nt] = t < 2 ? hi : M::pack(a - hf.x, b - hf.y);
+                if constexpr (NARROW) {                       // this lane's group is t: of columns 0 and 1, from lanes that have them
+                    const float own = t & 2 ? (t & 1 ? sum[3] : sum[2]) : (t & 1 ? sum[1] : sum[0]);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        qs[e] = __shfl_sync(0xffffffffu, own, e * 4 + t);
+                        cinit[0][0][e] = qs[e] * (t & 1 ? -72.f : -1032.f);
+                    }
+                } else {
+                    const float a = t & 1 ? sum[2] : sum[0], b = t & 1 ? sum[3] : sum[1];
+                    const uint32_t hi = M::pack(a, b);
+                    const float2 hf = M::unpack(hi);
+                    qsum[nt] = t < 2 ? hi : M::pack(a - hf.x, b - hf.y);
+                }
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int c2 = ct * NC + nt * 8 + 2 * t + e;
+                const int c2 = ct * NC + (NARROW ? e : nt * 8 + 2 * t + e);
                 const bool r2 = c2 < p.cols;
                 const int row2 = r2 ? c2 / p.group : first_row;
                 lim[nt][e] = pos0 + row2 + 1;
-                scale2[nt][e] = BITS == 4 ? kScale2 * __shfl_sync(0xffffffffu, unit, (2 * t + e) * 4) : kScale2;
-                slope[nt][e] = p.slopes && r2 ? __ldg(p.slopes + cur.h * p.group + (c2 - row2 * p.group)) * kLog2e / scale2[nt][e] : 0.f;
+                scale2[nt][e] = BITS == 4 ? kScale2 * __shfl_sync(0xffffffffu, unit, NARROW ? e * 4 : (2 * t + e) * 4) : kScale2;
+                slope[nt][e] = BIAS && r2 ? __ldg(p.slopes + cur.h * p.group + (c2 - row2 * p.group)) * kLog2e / scale2[nt][e] : 0.f;
                 mref[nt][e] = thr[nt][e] = -INFINITY;
                 base[nt][e] = lsum[nt][e] = 0.f;
             }
@@ -499,6 +517,34 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                             }
                         }
                         const uint32_t sc = src + Sh::SOFF + (u * 16 + kap) * 16;
+                        if constexpr (NARROW) {
+                            const float2 ss = M::unpack(__byte_perm(lds16(sc + 2 * t), lds16(sc + 128 + 2 * t), 0x5410));          // rows g and g + 8
+                            const float2 zz = M::unpack(__byte_perm(lds16(sc + 8 + 2 * t), lds16(sc + 136 + 2 * t), 0x5410));
+                            float acc[2][4];                  // two chains
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                                for (int w2 = 0; w2 < W / 2; ++w2) {
+                                    uint32_t a[4] = {wl[2 * w2], wh[2 * w2], wl[2 * w2 + 1], wh[2 * w2 + 1]};
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) {
+                                        if (j >= 2) a[i] >>= 8;
+                                        a[i] = j & 1 ? codes_hi(a[i]) : codes_lo(a[i]);
+                                    }
+                                    const uint32_t* b = qf[0][j * (W / 2) + w2];
+                                    float (&d)[4] = acc[j & 1];
+                                    if (w2 == 0 && j == 0) mma_h(d, a, b[0], b[1], cinit[0][0][0], cinit[0][0][1], cinit[0][0][0], cinit[0][0][1]);
+                                    else if (w2 == 0 && j == 1) mma_h(d, a, b[0], b[1], 0.f, 0.f, 0.f, 0.f);
+                                    else mma_h(d, a, b[0], b[1], d[0], d[1], d[2], d[3]);
+                                }
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                float v = fmaf(e < 2 ? ss.x : ss.y, acc[0][e] + acc[1][e], (e < 2 ? zz.x : zz.y) * qs[e & 1]);
+                                v += __shfl_xor_sync(0xffffffffu, v, 1);
+                                c[u][0][e] = v + __shfl_xor_sync(0xffffffffu, v, 2);
+                            }
+                            continue;
+                        }
                         const uint2 sl = lds64(sc), sh = lds64(sc + 128);
                         const float2 sl0 = M::unpack(sl.x), sl1 = M::unpack(sl.y), sh0 = M::unpack(sh.x), sh1 = M::unpack(sh.y);
                         const float fl[4] = {sl0.x, sl0.y, sl1.x, sl1.y}, fh[4] = {sh0.x, sh0.y, sh1.x, sh1.y};
@@ -536,7 +582,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                     }
                 }
                 // ---- bias, mask, reference (raw scores) ------------------------------------------------------------------------------
-                if (p.slopes) {
+                if constexpr (BIAS) {
 #pragma unroll
                     for (int u = 0; u < SUB; ++u)
 #pragma unroll
@@ -624,16 +670,22 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                     // The values' scales go into the weights, in fp32 before their one rounding; the codes stay exact.  A weight times a
                     // scale would leave fp16 at either end, so scales are taken relative to a power of two that only grows.
                     const uint32_t scales = src + Sh::SOFF + TK * 16;
-                    uint2 sl[SUB], sh[SUB];
+                    uint2 sl[SUB], sh[SUB];                           // (NARROW: of this lane's group alone, rows g and g + 8 side by side)
                     uint32_t big = 0;
 #pragma unroll
                     for (int u = 0; u < SUB; ++u) {
                         sl[u] = sh[u] = make_uint2(0u, 0u);
                         if (u == 0 || key0 + 16 * u < cur.klen) {                      // (else nothing was copied there)
-                            sl[u] = lds64(scales + (u * 16 + kap) * 16);
-                            sh[u] = lds64(scales + (u * 16 + kap) * 16 + 128);
+                            const uint32_t sc = scales + (u * 16 + kap) * 16;
+                            if constexpr (NARROW) {
+                                sl[u].x = __byte_perm(lds16(sc + 2 * t), lds16(sc + 128 + 2 * t), 0x5410);
+                                sh[u].x = __byte_perm(lds16(sc + 8 + 2 * t), lds16(sc + 136 + 2 * t), 0x5410);             // zero points
+                            } else {
+                                sl[u] = lds64(sc);
+                                sh[u] = lds64(sc + 128);
+                            }
                         }
-                        big = __vmaxu2(big, __vmaxu2(__vmaxu2(sl[u].x, sl[u].y), __vmaxu2(sh[u].x, sh[u].y)));     // (scales are not negative)
+                        big = __vmaxu2(big, NARROW ? sl[u].x : __vmaxu2(__vmaxu2(sl[u].x, sl[u].y), __vmaxu2(sh[u].x, sh[u].y)));     // (scales are not negative)
                     }
                     {
                         constexpr uint32_t top_exp = (0x7FFFu >> N::kExpShift) - 1;    // (NaN: as large as a number can be)
@@ -653,10 +705,18 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
 #pragma unroll
                     for (int u = 0; u < SUB; ++u) {
                         if (u > 0 && key0 + 16 * u >= cur.klen) break;
+                        uint32_t pf[NT][4][2];
+                        if constexpr (NARROW) {
+                            const float2 ss = M::unpack(sl[u].x), zz = M::unpack(sh[u].x);
+                            const float a = ss.x * unit, b = ss.y * unit;
+                            pf[0][0][0] = movmatrix_trans(Mma<__half>::pack(c[u][0][0] * a, c[u][0][1] * a));
+                            pf[0][0][1] = movmatrix_trans(Mma<__half>::pack(c[u][0][2] * b, c[u][0][3] * b));
+                            zo[0][0] = fmaf(c[u][0][0], zz.x, fmaf(c[u][0][2], zz.y, zo[0][0]));
+                            zo[0][1] = fmaf(c[u][0][1], zz.x, fmaf(c[u][0][3], zz.y, zo[0][1]));
+                        } else {
                         const float2 sl0 = M::unpack(sl[u].x), sl1 = M::unpack(sl[u].y), sh0 = M::unpack(sh[u].x), sh1 = M::unpack(sh[u].y);
                         const float fl[4] = {sl0.x * unit, sl0.y * unit, sl1.x * unit, sl1.y * unit};
                         const float fh[4] = {sh0.x * unit, sh0.y * unit, sh1.x * unit, sh1.y * unit};
-                        uint32_t pf[NT][4][2];
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -675,6 +735,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt)
                                 M::run(zo[nt], a, movmatrix_trans(M::pack(c[u][nt][0], c[u][nt][1])), movmatrix_trans(M::pack(c[u][nt][2], c[u][nt][3])));
+                        }
                         }
                         constexpr int VW = D / 64;            // code words of a value row that a lane weighs: channels g*D/8 + 8w ..
                         uint32_t w4[4][VW];
@@ -707,7 +768,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt) {
                                     float (&d)[4] = o[nt][w * 4 + j];
-                                    mma_h(d, a, pf[nt][j][0], pf[nt][j][1], d[0], d[1], d[2], d[3]);
+                                    mma_h(d, a, pf[nt][NARROW ? 0 : j][0], pf[nt][NARROW ? 0 : j][1], d[0], d[1], d[2], d[3]);
                                 }
                             }
                         }
@@ -727,7 +788,16 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) zg[j][e] = __shfl_sync(0xffffffffu, zo[nt][e], j * 4 + t);
+                    for (int e = 0; e < 2; ++e) {
+                        if constexpr (NARROW) {               // (this lane's group's, which is all that it will store)
+                            float z = zo[0][e];
+                            z += __shfl_xor_sync(0xffffffffu, z, 4);
+                            z += __shfl_xor_sync(0xffffffffu, z, 8);
+                            zg[j][e] = z + __shfl_xor_sync(0xffffffffu, z, 16);
+                        } else {
+                            zg[j][e] = __shfl_sync(0xffffffffu, zo[nt][e], j * 4 + t);
+                        }
+                    }
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -742,8 +812,8 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
                 l += __shfl_xor_sync(0xffffffffu, l, 4);
                 l += __shfl_xor_sync(0xffffffffu, l, 8);
                 l += __shfl_xor_sync(0xffffffffu, l, 16);
-                if (g == 0) {
-                    float* ml = s_ml + (warp * NC + nt * 8 + 2 * t + e) * 2;
+                if (g == 0 && (!NARROW || t == 0)) {
+                    float* ml = s_ml + (warp * NC + (NARROW ? e : nt * 8 + 2 * t + e)) * 2;
                     ml[0] = mref[nt][e] == -INFINITY ? -INFINITY : mref[nt][e] * scale2[nt][e];
                     ml[1] = l;
                 }
@@ -761,19 +831,21 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
 #pragma unroll
             for (int e = 0; e < 2; ++e)
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) top[e] = fmaxf(top[e], s_ml[(w * NC + nt * 8 + 2 * t + e) * 2]);
+                for (int w = 0; w < kWarps; ++w) top[e] = fmaxf(top[e], s_ml[(w * NC + (NARROW ? e : nt * 8 + 2 * t + e)) * 2]);
             float f[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) f[e] = mref[nt][e] == -INFINITY ? 1.f : exp2f(mref[nt][e] * scale2[nt][e] - top[e]);     // (no weight: zeros, or NaN)
             float mtop = -INFINITY, lall = 0.f;
+            const int lcol = NARROW ? mcol & 1 : nt * 8 + mcol;       // (NARROW: columns 2 to 7 are nobody's)
+            const bool there = !NARROW || mcol < 2;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) mtop = fmaxf(mtop, s_ml[(w * NC + nt * 8 + mcol) * 2]);
+            for (int w = 0; w < kWarps; ++w) mtop = fmaxf(mtop, s_ml[(w * NC + lcol) * 2]);
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-                const float mw = s_ml[(w * NC + nt * 8 + mcol) * 2], lw = s_ml[(w * NC + nt * 8 + mcol) * 2 + 1];
+                const float mw = s_ml[(w * NC + lcol) * 2], lw = s_ml[(w * NC + lcol) * 2 + 1];
                 lall += mw == -INFINITY ? lw : lw * exp2f(mw - mtop);
             }
-            const int col = ct * NC + nt * 8 + mcol;
+            const int col = ct * NC + lcol;
             const int row = col / p.group, hq = cur.h * p.group + (col - row * p.group);
             const float inv = lall == 0.f ? 0.f : 1.f / lall;
 #pragma unroll
@@ -784,31 +856,31 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int loc = BITS == 16 ? 16 * m + g + (e >= 2 ? 8 : 0) : 8 * g + m + (e >= 2 ? 4 : 0);
-                        mine[(2 * t + (e & 1)) * 68 + loc] = o[nt][r * 4 + m][e] * f[e & 1];
+                        if (!NARROW || m == t) mine[(NARROW ? e & 1 : 2 * t + (e & 1)) * 68 + loc] = o[nt][r * 4 + m][e] * f[e & 1];
                     }
                 __syncthreads();
                 float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) {
-                    const float4 b = *reinterpret_cast<const float4*>(s_merge + w * (8 * 68) + mcol * 68 + mloc);
+                    const float4 b = *reinterpret_cast<const float4*>(s_merge + w * (8 * 68) + (NARROW ? lcol : mcol) * 68 + mloc);
                     a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
                 }
                 const int d = BITS == 16 ? 64 * r + mloc : (mloc >> 3) * (D / 8) + 8 * r + (mloc & 7);
                 if (whole) {
-                    if (col < p.cols) {
+                    if (there && col < p.cols) {
                         uint2 w2;
                         w2.x = M::pack(a.x * inv, a.y * inv);
                         w2.y = M::pack(a.z * inv, a.w * inv);
                         *reinterpret_cast<uint2*>(p.out + ((((size_t)s * p.q_len + row) * p.H + hq) * D + d) * 2) = w2;
                     }
-                } else {
-                    *reinterpret_cast<float4*>(slot + (nt * 8 + mcol) * D + d) = a;
+                } else if (there) {
+                    *reinterpret_cast<float4*>(slot + lcol * D + d) = a;
                 }
                 __syncthreads();
             }
-            if (!whole && (tid & 15) == 0) {
-                slot[NC * D + nt * 8 + mcol] = mtop;
-                slot[NC * D + NC + nt * 8 + mcol] = lall;
+            if (!whole && there && (tid & 15) == 0) {
+                slot[NC * D + lcol] = mtop;
+                slot[NC * D + NC + lcol] = lall;
             }
         }
         if (!whole) {
@@ -827,6 +899,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     const int lcol = nt * 8 + mcol, col = ct * NC + lcol;
+                    if (lcol >= NC) break;
                     float top = -INFINITY, sum = 0.f;
                     float4 acc[D / 64];
 #pragma unroll
@@ -892,11 +965,11 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS>::CTAS) pages_sdpa
     cp_wait<0>();
 }
 
-template <typename T, int D, int NT, int BITS>
-cudaError_t launch_variant(const Params& p, int grid, bool pdl, cudaStream_t st) {
-    using Sh = Shape<D, NT, BITS>;
+template <typename T, int D, int NT, int BITS, bool NARROW, bool BIAS>
+cudaError_t launch_as(const Params& p, int grid, bool pdl, cudaStream_t st) {
+    using Sh = Shape<D, NT, BITS, NARROW>;
     static_assert((Sh::SMEM + 1024) * Sh::CTAS <= 233472, "shared memory of the CTAs of an SM");
-    auto kernel = pages_sdpa_kernel<T, D, NT, BITS>;
+    auto kernel = pages_sdpa_kernel<T, D, NT, BITS, NARROW, BIAS>;
     static std::atomic<bool> configured[64] = {};
     int dev = 0;
     cudaGetDevice(&dev);
@@ -920,11 +993,20 @@ cudaError_t launch_variant(const Params& p, int grid, bool pdl, cudaStream_t st)
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-// Columns of a tile: 8, or 16 where there are more; at head_dim 256 always 8 (16 would not fit the registers).
-int columns_of(int D, int cols) { return D == 256 || cols <= 8 ? 8 : 16; }
+template <typename T, int D, int NT, int BITS, bool NARROW = false>
+cudaError_t launch_variant(const Params& p, int grid, bool pdl, cudaStream_t st) {
+    return p.slopes ? launch_as<T, D, NT, BITS, NARROW, true>(p, grid, pdl, st) : launch_as<T, D, NT, BITS, NARROW, false>(p, grid, pdl, st);
+}
+
+// Columns of a tile: 8, or 16 where there are more; at head_dim 256 always 8 (16 would not fit the registers).  4 bits, one or two: 2.
+int columns_of(int D, int bits, int cols) { return bits == 4 && cols <= 2 ? 2 : D == 256 || cols <= 8 ? 8 : 16; }
 
 template <typename T, int BITS>
 cudaError_t launch_typed(int D, int nc, const Params& p, int grid, bool pdl, cudaStream_t st) {
+    if constexpr (BITS == 4) {
+        if (nc == 2) return D == 64 ? launch_variant<T, 64, 1, 4, true>(p, grid, pdl, st) : D == 128 ? launch_variant<T, 128, 1, 4, true>(p, grid, pdl, st)
+                                                                                                    : launch_variant<T, 256, 1, 4, true>(p, grid, pdl, st);
+    }
     if (D == 64) return nc == 8 ? launch_variant<T, 64, 1, BITS>(p, grid, pdl, st) : launch_variant<T, 64, 2, BITS>(p, grid, pdl, st);
     if (D == 128) return nc == 8 ? launch_variant<T, 128, 1, BITS>(p, grid, pdl, st) : launch_variant<T, 128, 2, BITS>(p, grid, pdl, st);
     return launch_variant<T, 256, 1, BITS>(p, grid, pdl, st);
@@ -943,7 +1025,7 @@ cudaError_t launch_pages_sdpa(const segkv_pages& h, const PageSdpaArgs& a, cudaS
     p.table_stride = a.table_stride; p.n = a.n; p.q_len = a.q_len; p.H = h.heads; p.Hkv = h.kv_heads; p.group = h.group;
     p.page_log = h.page_log; p.num_pages = h.num_pages;
     p.cols = a.q_len * h.group;
-    const int nc = columns_of(h.head_dim, p.cols);
+    const int nc = columns_of(h.head_dim, h.bits, p.cols);
     p.ctiles = (p.cols + nc - 1) / nc;
     const int grid = h.sm_count * ctas_per_sm(h.head_dim, nc, h.bits);
     if (h.dtype == SEGKV_BF16)
