@@ -57,8 +57,8 @@ int pack_log(const segkv_pages* h, bool slopes) {
 // knows, so that the ratio decides.  Measured (2560 keys, us, warp-level / tensor cores): head_dim 128, 32 x 4 heads, 2 sequences of 16
 // tokens 20.4 / 31.8, of 64 37.9 / 32.1, of 128 64.0 / 32.2, of 512 207 / 61.8, 16 of 5 39.5 / 33.3, 64 of 4 111 / 64.2; one of 64 at 32768 keys 168 /
 // 346; 32 x 32 heads, 4 of 32 45.6 / 34.1; head_dim 256, 16 x 16, 4 of 64 193 / 52.9; head_dim 64, 32 x 8, 4 of 64 43.9 / 31.6.
-bool many_rows(const segkv_pages* h, int n, int q_len, int pack) {
-    if (h->bits != 16) return false;
+bool many_rows(const segkv_pages* h, int n, int q_len, long long q_stride, int pack) {
+    if (h->bits != 16 || q_stride * q_len * 2 >= 1LL << 40) return false;           // (what a map's stride can hold)
     const long long cols = (long long)q_len * h->group, nc = h->head_dim == 256 ? 8 : 16, ctiles = (cols + nc - 1) / nc;
     if (ctiles < 2) return false;
     const long long items = (long long)n * (h->heads >> pack) * ((((long long)q_len << pack) + 127) / 128);
@@ -174,7 +174,7 @@ int segkv_pages_sdpa(segkv_pages_t h, int n, int q_len, const void* q, long long
     if (!rows_ok(q, q_stride, (long long)h->heads * h->head_dim) || !out || !aligned(out, 16) || !aligned(alibi_slopes, 4)) return SEGKV_EINVAL;
     if ((long long)n * q_len * h->group > 0x7FFFFFFFLL) return SEGKV_EINVAL;
     const int pack = pack_log(h, alibi_slopes != nullptr);
-    if (many_rows(h, n, q_len, pack)) {
+    if (many_rows(h, n, q_len, q_stride, pack)) {
         Dims d = {};
         d.batch = n; d.heads = h->heads >> pack; d.kv_heads = h->kv_heads; d.group = h->group >> pack; d.head_dim = h->head_dim; d.dtype = h->dtype;
         CUtensorMap tm_q;

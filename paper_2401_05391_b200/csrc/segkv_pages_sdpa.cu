@@ -205,14 +205,61 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    // ---- this CTA's run of blocks -------------------------------------------------------------------------------------------
+    // ---- this CTA's run of blocks ---------------------------------------------------------------------------------------------
+    // Block x of all `total` is CTA c's where total*c/G <= x < total*(c+1)/G.  Where there are few work groups that would leave some
+    // CTAs the end of one and the start of the next, one behind the other, with two meetings and two folds: 3 to 4 us, as
+    // long as three blocks.  So up to G/2 groups are cut into parts of `part` blocks each, one CTA a part, if that makes no CTA's run
+    // longer than three blocks more (16 bits, D 128: one request on 32 heads, 1152 keys, 11.0 -> 7.7 us, 8 x 8 heads x 2000 19.4 -> 16.0, 4 x 4 x 65536 with
+    // eight columns 88.0 -> 84.3).
     const int V = p.n * p.ctiles;
-    const int per = (V + kThreads - 1) / kThreads;
     int G = gridDim.x;
     const int cta = blockIdx.x;
-    unsigned long long x0, x1, total;
+    unsigned long long x0 = 0, total;
+    int blocks, part = 0;
     Cursor ld;
-    {
+    if (V <= 32) {                                            // a (sequence, column tile) per lane, every warp for itself
+        int klen = 0, nb = 0;
+        if (lane < V) extent<NC, KB>(p, lane, &klen, &nb, cta == 0);
+        auto scanned = [&](int v) {
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int u = __shfl_up_sync(0xffffffffu, v, o);
+                if (lane >= o) v += u;
+            }
+            return v;
+        };
+        const int all = __reduce_add_sync(0xffffffffu, nb);
+        total = (unsigned long long)all * p.Hkv;
+        // (quotients by reciprocals: of numbers below 2^19, half a unit off the border)
+        auto parts_of = [&](int size) { return (int)(((float)nb + ((float)size - 0.5f)) * (1.f / (float)size)); };
+        if (2 * V * p.Hkv <= G && total < (1u << 19)) {
+            const int least = (int)(((float)(unsigned)total + ((float)G - 0.5f)) * (1.f / (float)G));
+#pragma unroll 1
+            for (int k = 0; k < 4 && !part; ++k)
+                if ((int)__reduce_add_sync(0xffffffffu, parts_of(least + k)) * p.Hkv <= G) part = least + k;
+        }
+        const int units = part ? parts_of(part) : nb, incl = scanned(units);
+        if (part) {
+            x0 = cta;
+            if (cta >= __shfl_sync(0xffffffffu, incl, 31) * p.Hkv) return;             // (every thread)
+        } else {
+            if (total < (unsigned long long)G) G = (int)total;      // every CTA of a shared work group has to have a part
+            if (cta >= G) return;
+            x0 = total * cta / G;
+            blocks = (int)(total * (cta + 1) / G - x0);
+        }
+        const int src = __ffs(__ballot_sync(0xffffffffu, x0 < (unsigned long long)incl * p.Hkv)) - 1;
+        const int mine = __shfl_sync(0xffffffffu, units, src), before = __shfl_sync(0xffffffffu, incl, src) - mine;
+        const unsigned rest = (unsigned)(x0 - (unsigned long long)before * p.Hkv);
+        ld.v = src;
+        ld.h = (int)(rest / (unsigned)mine);
+        ld.b = (int)(rest - (unsigned)ld.h * (unsigned)mine) * (part ? part : 1);
+        ld.klen = __shfl_sync(0xffffffffu, klen, src);
+        ld.nb = __shfl_sync(0xffffffffu, nb, src);
+        ld.row = p.table + (long long)(src / p.ctiles) * p.table_stride;
+        if (part) blocks = min(part, ld.nb - ld.b);
+    } else {
+        const int per = (V + kThreads - 1) / kThreads;
         long long* s_scan = reinterpret_cast<long long*>(s_merge);
         long long mine = 0;
         const int v0 = min(tid * per, V), v1 = min(v0 + per, V);
@@ -236,10 +283,10 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
             all += s_scan[w];
         }
         total = (unsigned long long)all * p.Hkv;
-        if (total < (unsigned long long)G) G = (int)total;    // every CTA of a shared work group has to have a part
-        if (cta >= G) return;                                 // (every thread)
+        if (total < (unsigned long long)G) G = (int)total;
+        if (cta >= G) return;
         x0 = total * cta / G;
-        x1 = total * (cta + 1) / G;
+        blocks = (int)(total * (cta + 1) / G - x0);
         unsigned long long at = (unsigned long long)before * p.Hkv;
         if (mine > 0 && x0 >= at && x0 < at + (unsigned long long)mine * p.Hkv) {
             for (int v = v0;; ++v) {
@@ -262,7 +309,6 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
         enter<NC, KB>(p, ld);
     }
     Cursor cur = ld;
-    const int blocks = (int)(x1 - x0);
 
     // ---- copies -------------------------------------------------------------------------------------------------------------
     int pid[SUB];                                             // pages of the next tile to be copied
@@ -323,14 +369,31 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
         cp_commit();
     };
 
-    int copied = 0;
-    find_pages(ld);
+    static_assert(kStages == 3, "two tiles are copied ahead");
+    int copied = 1;
+    {
+        find_pages(ld);
+        const Cursor first = ld;
+        int pid0[SUB];
 #pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) {
-        if (copied < blocks) {
-            copy_tile(ld, i);
+        for (int u = 0; u < SUB; ++u) pid0[u] = pid[u];
+        if (blocks > 1) {                                     // (both tiles' pages are asked for together)
+            advance<NC, KB>(p, ld, V);
+            find_pages(ld);
+        }
+        int pid1[SUB];
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            pid1[u] = pid[u];
+            pid[u] = pid0[u];
+        }
+        copy_tile(first, 0);
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) pid[u] = pid1[u];
+        if (blocks > 1) {
+            copy_tile(ld, 1);
             ++copied;
-            if (copied < blocks) {
+            if (blocks > 2) {
                 advance<NC, KB>(p, ld, V);
                 find_pages(ld);
             }
@@ -820,9 +883,15 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
             }
         __syncthreads();
         // which CTAs share the work group: the one where it begins uses its second slot, the others their first
-        unsigned long long gbase = x - (unsigned)cur.b;       // (x is the index of block cur.b)
-        const int c0 = whole ? cta : (int)(((gbase + 1) * G - 1) / total);
-        const int c1 = whole ? cta : (int)(((gbase + cur.nb) * G - 1) / total);
+        int c0 = cta, c1 = cta;
+        if (part) {
+            c0 -= cur.b / part;
+            c1 = c0 + (cur.nb + part - 1) / part - 1;
+        } else if (!whole) {
+            const unsigned long long gbase = x - (unsigned)cur.b;                      // (x is the index of block cur.b)
+            c0 = (int)(((gbase + 1) * G - 1) / total);
+            c1 = (int)(((gbase + cur.nb) * G - 1) / total);
+        }
         float* slot = p.ws + ((size_t)cta * 2 + (cta == c0 ? 1 : 0)) * Sh::SLOT;
         const int mcol = tid >> 4, mloc = (tid & 15) * 4;     // this thread's column (of eight) and channels (of 64) in each round
 #pragma unroll

@@ -119,7 +119,8 @@ def test_attention_of_many_rows(shape, dtype):
 
 
 @pytest.mark.parametrize("bits,dtype,H,Hkv,D,T,lens", [
-    (16, F16, 4, 1, 128, 1, [20011]), (4, F16, 4, 1, 128, 1, [20011]), (16, BF16, 16, 2, 64, 1, [9999, 3, 70]),
+    (16, F16, 4, 1, 128, 1, [20011]), (4, F16, 2, 2, 128, 1, [3001, 64, 900]), (4, BF16, 1, 1, 256, 1, [8000]), (4, F16, 40, 40, 64, 1, [777] * 9),
+    (16, F16, 3, 3, 128, 1, [200 + 37 * i for i in range(40)]), (16, BF16, 80, 80, 64, 1, [500, 0, 1300]), (4, F16, 4, 1, 128, 1, [20011]), (16, BF16, 16, 2, 64, 1, [9999, 3, 70]),
     (4, BF16, 16, 2, 256, 1, [5000, 12000]), (4, F16, 9, 1, 64, 2, [30001]), (16, F16, 2, 2, 256, 1, [7777]),
     (4, BF16, 8, 1, 128, 4, [4097] * 3)])
 def test_work_groups_shared_by_many_ctas(bits, dtype, H, Hkv, D, T, lens):
@@ -378,6 +379,22 @@ def test_bad_tables_are_flagged(bits):
         c.append(k, k, table, torch.tensor([0, value], dtype=torch.int32, device="cuda"), torch.tensor([0, 1], dtype=torch.int32, device="cuda"))
         assert c.get_error() == sk.SEGKV_DEV_BAD_PAGE
         assert all(torch.equal(a, b) for a, b in zip(before, (c.k_pages, c.v_pages)))
+    c.destroy()
+
+
+def test_bad_tables_are_flagged_where_rows_are_many():
+    c, table, lens = filled(4, 2, 64, 16, [300, 280], F16, 16, 105)
+    q = randn(2, 256, 4, 64, dtype=F16, g=gen(106))
+    good = c.sdpa(q, table, lens)
+    for value in (-1, c.num_pages, 2 ** 31 - 1, -2 ** 31):
+        bad = table.clone()
+        bad[1, 3] = value
+        out = c.sdpa(q, bad, lens)
+        assert c.get_error() == sk.SEGKV_DEV_BAD_PAGE and torch.equal(out[0], good[0]) and torch.isfinite(out[1]).all()
+    for value in (-5, 305, 2 ** 31 - 1, -2 ** 31):
+        out = c.sdpa(q, table, torch.tensor([300, value], dtype=torch.int32, device="cuda"))
+        assert c.get_error() == sk.SEGKV_DEV_BAD_PAGE and torch.equal(out[0], good[0])
+        assert not out[1].any() if value < 0 else torch.isfinite(out[1]).all()
     c.destroy()
 
 

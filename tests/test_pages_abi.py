@@ -80,3 +80,45 @@ def test_runs_of_blocks_cover_every_work_group_once(seed):
         seen += nb
         base += nb
     assert seen == total
+
+
+def _parts(nb, size):
+    """ceil(nb / size) as the kernel takes it: in fp32, by a reciprocal, half a unit off the border."""
+    f = np.float32
+    return int((f(nb) + (f(size) - f(0.5))) * (f(1) / f(size)))
+
+
+@pytest.mark.parametrize("seed", range(30))
+def test_parts_of_few_work_groups_fit_the_grid(seed):
+    """The other schedule restated: where groups are few, every CTA takes one part of one group, and all blocks are taken once."""
+    rng = np.random.default_rng(100 + seed)
+    G = int(rng.choice([148, 296, 444]))
+    V = int(rng.integers(1, 33))
+    heads = int(rng.integers(1, max(2, G // (2 * V) + 1)))
+    nbs = [int(x) for x in rng.integers(1, rng.choice([3, 40, 2000]), size=V)]
+    total = sum(nbs) * heads
+    if 2 * V * heads > G or total >= 1 << 19:
+        pytest.skip("not its to take")
+    least = int((np.float32(total) + (np.float32(G) - np.float32(0.5))) * (np.float32(1) / np.float32(G)))
+    part = next((least + k for k in range(4) if sum(_parts(nb, least + k) for nb in nbs) * heads <= G), 0)
+    if not part:
+        return                                                 # (the runs of the other schedule)
+    assert all(_parts(nb, part) == -(-nb // part) for nb in nbs)
+    taken, cta = set(), 0
+    for v, nb in enumerate(nbs):
+        units = _parts(nb, part)
+        for h in range(heads):
+            for u in range(units):
+                blocks = min(part, nb - u * part)
+                assert 0 < blocks <= part and cta < G
+                taken |= {(v, h, u * part + b) for b in range(blocks)}
+                cta += 1
+    assert len(taken) == total
+
+
+def test_quotients_by_reciprocals_are_right_below_2_to_the_19():
+    rng = np.random.default_rng(7)
+    for size in [1, 2, 3, 5, 7, 9, 13, 100, 1771, 4097, 99991, 300007]:
+        for nb in [*range(1, 50), *(size * k + d for k in (1, 2, 3, 17, 523) for d in (-1, 0, 1)), *rng.integers(1, 1 << 19, 200)]:
+            if 0 < nb < 1 << 19:
+                assert _parts(int(nb), size) == -(-int(nb) // size), (nb, size)
