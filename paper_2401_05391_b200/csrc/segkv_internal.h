@@ -236,6 +236,8 @@ struct PrefillArgs {
     // dims, count packed rows and groups of packed heads (see the kernel)
     const int32_t *table = nullptr, *lens = nullptr;
     int table_stride = 0, page_log = 0, num_pages = 0, q_len = 0, pack_log = 0, box_log = 0;
+    const void *kp4 = nullptr, *vp4 = nullptr;       // 4-bit pages (then no maps but the query's), bytes of a page and of a head's rows in it
+    size_t page_bytes = 0, head_bytes = 0;
 };
 // A 4-D tensor map over 16-bit elements in coordinates (d, head, token, request): extents, element strides of the last three, box
 // in heads and tokens (and 64 elements: one 128-byte swizzle span).  `what` names the array in the error text.

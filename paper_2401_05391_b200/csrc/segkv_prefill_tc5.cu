@@ -78,6 +78,9 @@ struct Tc5Params {
     int table_stride, page_log, num_pages, q_len;
     int pack_log;            // query heads of a kv head side by side in the rows, as a power of two
     int box_log;             // rows of a page that one copy brings, as a power of two
+    const char *kp4, *vp4;   // 4-bit pages (MODE 4), bytes of a page and of a head's rows in it
+    unsigned long long page_bytes;
+    uint32_t head_bytes;
     int dbg_skip;            // test aid: one softmax thread leaves out one barrier arrival, so that a wait runs out
     unsigned long long wait_ns;   // limit of every bounded wait
 };
@@ -91,13 +94,14 @@ template <typename T> constexpr float kWeightMax = SplitP<T>::value ? 256.f : 32
 
 // Shape of one instantiation: head_dim D (64, 128 or 256), KEYS keys per K/V tile, NG groups of
 // 128 query rows per CTA.  head_dim 256 leaves tensor memory for one group and 64-key tiles only.
-template <int D_, int KEYS_, int NG_>
+// DQ: warps that make the K and V tiles from 4-bit rows (MODE 4), half of them each.
+template <int D_, int KEYS_, int NG_, int DQ_ = 0>
 struct Tc5Layout {
-    static constexpr int D = D_, KEYS = KEYS_, NG = NG_;
+    static constexpr int D = D_, KEYS = KEYS_, NG = NG_, DQ = DQ_;
     static constexpr int NB = NG == 1 ? 2 : 1;                   // S buffers per group
-    static constexpr int TPR = D == 256 ? 2 : 4 / NG;            // softmax threads per query row
+    static constexpr int TPR = D == 256 || DQ ? 2 : 4 / NG;      // softmax threads per query row
     static constexpr int kSoftWarps = 4 * TPR * NG;
-    static constexpr int kThreads = 32 * (kSoftWarps + 4);       // and TMA loads, MMAs, TMA stores, one idle (it costs no registers)
+    static constexpr int kThreads = 32 * (kSoftWarps + (DQ ? 2 + DQ : 4));      // and TMA loads, MMAs, TMA stores, one idle (it costs no registers)
     static constexpr int kDBoxes = D / 64;                       // 64-element (128-byte) column blocks of a row
     static constexpr int kBoxRows = D == 256 ? 32 : 64;          // rows of one TMA box of the prompt segment's tensor map
     static constexpr int kBoxBytes = kBoxRows * 128;
@@ -224,14 +228,19 @@ __device__ __forceinline__ uint64_t weigh16(const uint32_t* sr, float scale2, fl
 //   * a K or V tile is copied page by page (pieces of at least 16 rows, all of one (page, kv head)) through a map of the pool in
 //     coordinates (d, kv head, row, page); what lies wholly behind the sequence is asked for behind the page's last row, which
 //     gives zeros, and the rows of the last page that do not exist, whatever they hold, are zeroed in the V tile by the MMA
-//     warp (a weight of 0 times a NaN is a NaN; their scores are masked).
+//     warp (a weight of 0 times a NaN is a NaN; their scores are masked);
+// 4: the same over 4-bit pages: eight warps make the tiles, four for K and four for V.  A lane has a row (half a row at head_dim 256), asks
+// for the next tile's codes and scales while it works on this one's, turns them into the 16-bit values that they stand for
+// (z + s (c - 8), rounded once) and stores them where the TMA would: 2.3 instructions a code, once for all 128 rows, under the softmax of the
+// tile before.  Rows that do not exist are zeros.
 template <typename T, typename L, int MODE>
 __global__ void __launch_bounds__(L::kThreads, 1)
 prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_k_seg,
                    const __grid_constant__ CUtensorMap tm_v_seg, const Tc5Params p) {
     constexpr int NG = L::NG, NB = L::NB, TPR = L::TPR, SK = L::kStagesK, SV = L::kStagesV;
-    constexpr bool STORE = MODE == 1, RAGGED = MODE == 2, PAGED = MODE == 3;
+    constexpr bool STORE = MODE == 1, RAGGED = MODE == 2, PAGED = MODE >= 3, FOUR = MODE == 4;
+    static_assert(FOUR == (L::DQ > 0), "warps for the tiles of 4-bit pages");
     constexpr bool kSplitP = sizeof(typename SplitP<T>::yes) != 0 && SplitP<T>::value;
     constexpr int kD = L::D, kKeys = L::KEYS, kTileKV = L::kTileKV, kColTile = L::kColTile;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -310,11 +319,11 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     if (tid == 0) {
         // a stage is released by the MMAs that read it and, when tiles are stored on, by the store thread
         for (int s = 0; s < SK; ++s) {
-            mbar_init(kfull0 + 8 * s, 1);
+            mbar_init(kfull0 + 8 * s, FOUR ? L::DQ / 2 : 1);
             mbar_init(kempty0 + 8 * s, STORE ? 2 : 1);
         }
         for (int s = 0; s < SV; ++s) {
-            mbar_init(vfull0 + 8 * s, 1);
+            mbar_init(vfull0 + 8 * s, FOUR ? L::DQ / 2 : 1);
             mbar_init(vempty0 + 8 * s, STORE ? 2 : 1);
         }
         for (int g = 0; g < NG; ++g) {
@@ -404,7 +413,7 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                         tma_load_4d(dst + cb * kBoxQ, &tm_q, cb * 64, PAGED ? h << p.pack_log : h,
                                     PAGED ? ((qt * NG + g) * kRows) >> p.pack_log : (qt * NG + g) * kRows, b, qfull);
                 }
-                for (int i = 0; i < nkt && ok; ++i, ++tp) {
+                for (int i = 0; i < nkt && ok && !FOUR; ++i, ++tp) {
                     const int kt = tile_at(i, nkt);
                     const uint32_t sk = tp % SK, sv = tp % SV;
                     int ids[kMaxPieces];
@@ -434,11 +443,112 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             }
             if (!ok) s_abort = 1;
             // no copy may land after the CTA has gone (all have, unless a wait ran out somewhere)
+            // (MODE 4: only queries were copied; tk and tp are 0)
             for (uint32_t k = tk > (uint32_t)SK ? tk - SK : 0; k < tk; ++k) (void)mbar_wait(kfull0 + 8 * (k % SK), (k / SK) & 1, p.wait_ns);
             for (uint32_t k = tp > (uint32_t)SV ? tp - SV : 0; k < tp; ++k) (void)mbar_wait(vfull0 + 8 * (k % SV), (k / SV) & 1, p.wait_ns);
 #pragma unroll
             for (int g = 0; g < NG; ++g)
                 if (qi[g] > 0) (void)mbar_wait(gbar0 + kGB * g + 32, (qi[g] - 1) & 1, p.wait_ns);
+        }
+    } else if (FOUR && warp >= L::kSoftWarps + 2) {
+        if constexpr (FOUR) {
+            // ------------------------------- tiles from 4-bit pages -------------------------------
+            constexpr int DW = L::DQ / 2, PARTS = 32 * DW / kKeys;       // warps of K and of V; lanes of a row
+            constexpr int CH = kD / 32 / PARTS;                          // 16-byte chunks of codes for a lane
+            const int dw = (warp - L::kSoftWarps - 2) % DW;
+            const bool is_v = warp - L::kSoftWarps - 2 >= DW;
+            const int row = (dw * 32 + lane) % kKeys, part = (dw * 32 + lane) / kKeys;
+            const char* const pages = is_v ? p.vp4 : p.kp4;
+            const uint32_t full0 = is_v ? vfull0 : kfull0, empty0 = is_v ? vempty0 : kempty0, stages = is_v ? SV : SK;
+            const uint32_t ring = smem_u32(is_v ? v_ring : k_ring);
+            struct Tile { int kt, b, kvh, len, pid; };                   // kt -1: no more
+            int j = -1, i = 0, nkt = 0, b = 0, kvh = 0;
+            // the next tile of this CTA, its row's page asked for
+            auto next_tile = [&]() -> Tile {
+                while (i >= nkt) {
+                    if (++j >= p.rounds) return Tile{-1, 0, 0, 0, 0};
+                    const int w = round_item(j);
+                    i = nkt = 0;
+                    if (w >= n_items) continue;
+                    const int qt = item_qt(w), hb = w % hb_count;
+                    b = hb / p.H;
+                    kvh = (hb % p.H) / p.G;
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) nkt = max(nkt, group_tiles(qt, g, request_len(b)));
+                }
+                Tile t{tile_at(i, nkt), b, kvh, request_len(b), 0};
+                ++i;
+                const int key = t.kt * kKeys + row;
+                if (key < t.len) t.pid = p.table[(long long)b * p.table_stride + (key >> p.page_log)];
+                return t;
+            };
+            uint4 code[2][CH], scale[2];
+            auto load = [&](const Tile& t, uint4 (&c)[CH], uint4& s) {
+                const int key = t.kt * kKeys + row;
+                s = make_uint4(0u, 0u, 0u, 0u);                          // (a row that does not exist stands for zeros)
+                if (t.kt < 0 || key >= t.len) return;
+                int pid = t.pid;
+                if ((unsigned)pid >= (unsigned)p.num_pages) {
+                    atomicOr(p.err_word, SEGKV_DEV_BAD_PAGE);
+                    pid = 0;
+                }
+                const uint32_t in_page = (uint32_t)key & ((1u << p.page_log) - 1);
+                const char* blk = pages + (unsigned long long)(uint32_t)pid * p.page_bytes + (unsigned long long)t.kvh * p.head_bytes;
+                const uint4* src = reinterpret_cast<const uint4*>(blk + in_page * (uint32_t)(kD / 2)) + part * CH;
+#pragma unroll
+                for (int k = 0; k < CH; ++k) c[k] = src[k];
+                s = *reinterpret_cast<const uint4*>(blk + (kD / 2u << p.page_log) + in_page * 16);
+            };
+            constexpr uint32_t magic = kSplitP ? 0x43004300u : 0x64006400u, off = kSplitP ? 0x43084308u : 0x64086408u;      // 128 or 1024; and 8 more
+            using T2 = typename std::conditional<kSplitP, __nv_bfloat162, __half2>::type;
+            auto value = [&](uint32_t two, uint32_t s, uint32_t z) -> uint32_t {      // two codes in bits 0-3 and 16-19
+                uint32_t x;
+                asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(x) : "r"(two), "r"(0x000F000Fu), "r"(magic));
+                const T2 c = __hsub2(*reinterpret_cast<const T2*>(&x), *reinterpret_cast<const T2*>(&off));
+                const T2 v = __hfma2(c, *reinterpret_cast<const T2*>(&s), *reinterpret_cast<const T2*>(&z));
+                return *reinterpret_cast<const uint32_t*>(&v);
+            };
+            uint32_t tp = 0;
+            bool ok = true;
+            auto store = [&](const uint4 (&c)[CH], const uint4& s) {
+                const uint32_t st = tp % stages;
+                ok = __all_sync(0xffffffffu, mbar_wait_hot(empty0 + 8 * st, ((tp / stages) & 1) ^ 1, p.wait_ns));
+                if (!ok) return;
+                const uint32_t to = ring + st * (uint32_t)kTileKV + row * 128;
+#pragma unroll
+                for (int k = 0; k < CH; ++k) {
+                    const uint32_t w4[4] = {c[k].x, c[k].y, c[k].z, c[k].w};
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const uint32_t w = w4[u], h = w >> 4;
+                        const int at = (part * CH + k) * 4 + u;          // 16-byte chunk of the row's values
+                        const uint32_t dst = to + (at >> 3) * (uint32_t)kColTile + (((at & 7) ^ (row & 7)) << 4);
+                        const uint32_t v0 = value(__byte_perm(w, h, 0x0400), s.x, s.z), v1 = value(__byte_perm(w, h, 0x0501), s.y, s.w);
+                        const uint32_t v2 = value(__byte_perm(w, h, 0x0602), s.x, s.z), v3 = value(__byte_perm(w, h, 0x0703), s.y, s.w);
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(v0), "r"(v1), "r"(v2), "r"(v3) : "memory");
+                    }
+                }
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(full0 + 8 * st);
+                ++tp;
+            };
+#pragma unroll
+            for (int k = 0; k < CH; ++k) code[0][k] = code[1][k] = make_uint4(0u, 0u, 0u, 0u);
+            Tile t0 = next_tile();
+            load(t0, code[0], scale[0]);
+            Tile t1 = t0.kt < 0 ? t0 : next_tile();
+            while (t0.kt >= 0 && ok) {                                   // (two tiles a turn, so that registers have fixed names)
+                Tile t2 = t1.kt < 0 ? t1 : next_tile();
+                load(t1, code[1], scale[1]);
+                store(code[0], scale[0]);
+                if (t1.kt < 0 || !ok) break;
+                t0 = t2;
+                t1 = t2.kt < 0 ? t2 : next_tile();
+                load(t0, code[0], scale[0]);
+                store(code[1], scale[1]);
+            }
+            if (!ok) s_abort = 1;
         }
     } else if (warp == L::kSoftWarps + 2) {
         if (STORE && lane == 0) {
@@ -576,7 +686,7 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     const uint64_t vd = dv + (v_lo0 + vst * (uint32_t)(kTileKV >> 4));
                     ok = wait(vfull0 + 8 * vst, vph);
                     if (!ok) break;
-                    if (PAGED && (kt + 1) * kKeys > nb) {         // rows of the last page that do not exist
+                    if (PAGED && !FOUR && (kt + 1) * kKeys > nb) {       // rows of the last page that do not exist
                         const int v0 = nb - kt * kKeys, v1 = ((v0 + (1 << p.box_log) - 1) >> p.box_log) << p.box_log;
                         uint8_t* tile = v_ring + (size_t)vst * kTileKV;
                         for (int i = v0 * 8 + lane; i < v1 * 8; i += 32)
@@ -976,6 +1086,7 @@ bool deal_in_pairs(const Dims& d, int prompt_len, bool biased, int nqt, int bpw,
 template <typename T, typename L>
 cudaError_t launch_tc5(const Dims& d, const PrefillArgs& a, Tc5Params p, int sms, cudaStream_t st) {
     constexpr int NG = L::NG;
+    constexpr bool FOUR = L::DQ > 0;
     // Never two CTAs on one SM: each allocates all of tensor memory and keeps it while it walks
     // its items, so a second one would wait for it inside tcgen05.alloc.
     constexpr size_t smem = L::kBytes > 120 * 1024 ? L::kBytes : 120 * 1024;
@@ -983,13 +1094,18 @@ cudaError_t launch_tc5(const Dims& d, const PrefillArgs& a, Tc5Params p, int sms
     int dev = 0;
     cudaGetDevice(&dev);
     if (dev >= 0 && dev < 64 && !configured[dev]) {
-        cudaError_t e = cudaFuncSetAttribute(prefill_tc5_kernel<T, L, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(prefill_tc5_kernel<T, L, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(prefill_tc5_kernel<T, L, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(prefill_tc5_kernel<T, L, 3>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        cudaError_t e = cudaSuccess;
+        if constexpr (FOUR) {
+            e = cudaFuncSetAttribute(prefill_tc5_kernel<T, L, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        } else {
+            e = cudaFuncSetAttribute(prefill_tc5_kernel<T, L, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (e == cudaSuccess)
+                e = cudaFuncSetAttribute(prefill_tc5_kernel<T, L, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (e == cudaSuccess)
+                e = cudaFuncSetAttribute(prefill_tc5_kernel<T, L, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (e == cudaSuccess)
+                e = cudaFuncSetAttribute(prefill_tc5_kernel<T, L, 3>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        }
         if (e != cudaSuccess) return e;
         configured[dev] = true;
     }
@@ -1022,10 +1138,14 @@ cudaError_t launch_tc5(const Dims& d, const PrefillArgs& a, Tc5Params p, int sms
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = a.pdl ? 1 : 0;
-    if (p.table) return cudaLaunchKernelEx(&cfg, prefill_tc5_kernel<T, L, 3>, *a.tm_q, *a.tm_k, *a.tm_v, *a.tm_k, *a.tm_v, p);
-    if (store) return cudaLaunchKernelEx(&cfg, prefill_tc5_kernel<T, L, 1>, *a.tm_q, *a.tm_k_src, *a.tm_v_src, *a.tm_k, *a.tm_v, p);
-    if (p.plens) return cudaLaunchKernelEx(&cfg, prefill_tc5_kernel<T, L, 2>, *a.tm_q, *a.tm_k, *a.tm_v, *a.tm_k, *a.tm_v, p);
-    return cudaLaunchKernelEx(&cfg, prefill_tc5_kernel<T, L, 0>, *a.tm_q, *a.tm_k, *a.tm_v, *a.tm_k, *a.tm_v, p);
+    if constexpr (FOUR) {
+        return cudaLaunchKernelEx(&cfg, prefill_tc5_kernel<T, L, 4>, *a.tm_q, *a.tm_q, *a.tm_q, *a.tm_q, *a.tm_q, p);       // (no maps but the query's)
+    } else {
+        if (p.table) return cudaLaunchKernelEx(&cfg, prefill_tc5_kernel<T, L, 3>, *a.tm_q, *a.tm_k, *a.tm_v, *a.tm_k, *a.tm_v, p);
+        if (store) return cudaLaunchKernelEx(&cfg, prefill_tc5_kernel<T, L, 1>, *a.tm_q, *a.tm_k_src, *a.tm_v_src, *a.tm_k, *a.tm_v, p);
+        if (p.plens) return cudaLaunchKernelEx(&cfg, prefill_tc5_kernel<T, L, 2>, *a.tm_q, *a.tm_k, *a.tm_v, *a.tm_k, *a.tm_v, p);
+        return cudaLaunchKernelEx(&cfg, prefill_tc5_kernel<T, L, 0>, *a.tm_q, *a.tm_k, *a.tm_v, *a.tm_k, *a.tm_v, p);
+    }
 }
 
 template <typename T>
@@ -1033,6 +1153,14 @@ cudaError_t dispatch_tc5(const Dims& d, const PrefillArgs& a, const Tc5Params& p
     // two row groups per CTA once there are enough 256-row items to fill the machine a few times over
     const long items2 = (long)((a.prompt_len + 2 * kRows - 1) / (2 * kRows)) * d.heads * d.batch;
     const bool two = a.row_groups ? a.row_groups == 2 : items2 >= 2L * sms;
+    if (a.kp4) {
+        switch (d.head_dim) {
+            case 64: return launch_tc5<T, Tc5Layout<64, 128, 1, 8>>(d, a, p, sms, st);
+            case 128: return launch_tc5<T, Tc5Layout<128, 128, 1, 8>>(d, a, p, sms, st);
+            case 256: return launch_tc5<T, Tc5Layout<256, 64, 1, 8>>(d, a, p, sms, st);
+            default: return cudaErrorInvalidValue;
+        }
+    }
     switch (d.head_dim) {
         case 64:
             return two ? launch_tc5<T, Tc5Layout<64, 128, 2>>(d, a, p, sms, st)
@@ -1059,6 +1187,7 @@ cudaError_t launch_prefill_tc5(const Dims& d, const PrefillArgs& a, cudaStream_t
     p.scale2 = 0.f; p.idesc_qk = p.idesc_pv = 0; p.snake = 0; p.paired = 0; p.rounds = 0;
     p.table = a.table; p.lens = a.lens; p.table_stride = a.table_stride; p.page_log = a.page_log; p.num_pages = a.num_pages;
     p.q_len = a.q_len; p.pack_log = a.pack_log; p.box_log = a.box_log;
+    p.kp4 = (const char*)a.kp4; p.vp4 = (const char*)a.vp4; p.page_bytes = a.page_bytes; p.head_bytes = (uint32_t)a.head_bytes;
     p.dbg_skip = a.dbg_skip ? 1 : 0;
     p.wait_ns = a.wait_ns ? a.wait_ns : kWaitLimitNs;
     int sms = 148;

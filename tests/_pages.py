@@ -80,14 +80,16 @@ def sequence(cache, table, b, length):
     return out
 
 
-def attention(cache, q, table, lens, slopes=None):
+def attention(cache, q, table, lens, slopes=None, rounded=False):
     """(out, tolerance) in 64 bits, [n, q_len, heads, D].
 
     Tolerance of a kernel that holds scores, sums and accumulators in fp32 and rounds weights once and the output once to the dtype
     (u = half a step): u |out| for the output and u sum p |v| for the weights, v in the parts that are summed; a score's fp32
     error ds moves a weight by a factor e^ds, 2 ds sum p |v| at most with the sum it is divided by.  ds: D + 16 additions, each off by at most
     2^-22 of the terms' absolute sum (a tensor core cuts where fp32 would round); with 4-bit keys the terms are q (magic + code), up to 1040
-    steps of the scale in fp16 and 144 in bf16.  ALiBi adds 2^-22 of its own size.  1e-5: exponentials, rescaling and the merge of splits."""
+    steps of the scale in fp16 and 144 in bf16.  ALiBi adds 2^-22 of its own size.  1e-5: exponentials, rescaling and the merge of splits.
+    rounded: a kernel for many rows takes keys and values as the 16-bit numbers nearest to what 4-bit rows stand for: u |k| in the terms of a
+    score, u |v| in those of the sum."""
     n, T, H, D = q.shape
     u = torch.finfo(cache.dtype).eps / 2
     G = H // cache.kv_heads
@@ -107,6 +109,8 @@ def attention(cache, q, table, lens, slopes=None):
             if kstep is not None:
                 terms = terms + qh.abs().sum(-1, keepdim=True) * kstep[h // G][:, 0][None] * (1040.0 if cache.dtype == torch.float16 else 144.0)
             ds = (D + 16) * 2.0 ** -22 * terms / math.sqrt(D)
+            if rounded:
+                ds = ds + u * (qh.abs() @ k[h // G].abs().T) / math.sqrt(D)
             if slopes is not None:
                 x = x + slopes[h].double() * away
                 ds = ds + 2.0 ** -22 * (slopes[h].double() * away).abs()
@@ -116,7 +120,7 @@ def attention(cache, q, table, lens, slopes=None):
             worst = torch.where(p > 0, ds, torch.zeros_like(ds))
             worst = (p * worst).sum(-1, keepdim=True) + worst * 1.0                                      # (of the sum, and of the weight)
             out[b, :, h] = p @ v[h // G]
-            tol[b, :, h] = u * out[b, :, h].abs() + (p * (1.05 * u + 1e-5 + 2 * worst.clamp(max=1.0))) @ size[h // G]
+            tol[b, :, h] = u * out[b, :, h].abs() + (p * ((2.05 if rounded else 1.05) * u + 1e-5 + 2 * worst.clamp(max=1.0))) @ size[h // G]
             tol[b, :, h] += L * 2.0 ** -30 * size[h // G].amax() + (2.0 ** -25 if cache.dtype == torch.float16 else 0.0)
     return out, tol
 

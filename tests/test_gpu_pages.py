@@ -99,19 +99,20 @@ MANY = [
 ]
 
 
+@pytest.mark.parametrize("bits", [16, 4])
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("shape", MANY, ids=lambda s: "x".join(map(str, s[:5])))
-def test_attention_of_many_rows(shape, dtype):
+def test_attention_of_many_rows(shape, dtype, bits):
     H, Hkv, D, ps, T, lens = shape
     seed = 7 * H + D + ps + T
-    c, table, n_lens = filled(H, Hkv, D, ps, lens, dtype, 16, seed, poison=True)
+    c, table, n_lens = filled(H, Hkv, D, ps, lens, dtype, bits, seed, poison=True)
     for alibi in (False, True):
         x = randn(len(lens), T, H + 2, D, dtype=dtype, g=gen(seed + 1))
         q = x[:, :, 1:H + 1] if D == 64 else x[:, :, :H].contiguous()
         slopes = wl.alibi_slopes(H).cuda() if alibi else None
         out = torch.full((len(lens), T, H, D), math.nan, dtype=dtype, device="cuda")
         c.sdpa(q, table, n_lens, out, slopes)
-        pg.check(out, *pg.attention(c, q, table, lens, slopes))
+        pg.check(out, *pg.attention(c, q, table, lens, slopes, rounded=bits == 4))
         again = c.sdpa(q, table, n_lens, None, slopes)
         assert torch.equal(out, again)
     assert c.get_error() == 0
@@ -382,8 +383,9 @@ def test_bad_tables_are_flagged(bits):
     c.destroy()
 
 
-def test_bad_tables_are_flagged_where_rows_are_many():
-    c, table, lens = filled(4, 2, 64, 16, [300, 280], F16, 16, 105)
+@pytest.mark.parametrize("bits", [16, 4])
+def test_bad_tables_are_flagged_where_rows_are_many(bits):
+    c, table, lens = filled(4, 2, 64, 16, [300, 280], F16, bits, 105)
     q = randn(2, 256, 4, 64, dtype=F16, g=gen(106))
     good = c.sdpa(q, table, lens)
     for value in (-1, c.num_pages, 2 ** 31 - 1, -2 ** 31):
