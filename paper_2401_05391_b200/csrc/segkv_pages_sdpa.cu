@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
     // ---- this CTA's run of blocks ---------------------------------------------------------------------------------------------
     // Block x of all `total` is CTA c's where total*c/G <= x < total*(c+1)/G.  Where there are few work groups that would leave some
     // CTAs the end of one and the start of the next, one behind the other, with two meetings and two folds: 3 to 4 us, as
-    // long as three blocks.  So up to G/2 groups are cut into parts of `part` blocks each, one CTA a part, if that makes no CTA's run
+    // long as three blocks.  So up to G groups are cut into parts of `part` blocks each, one CTA a part, if that makes no CTA's run
     // longer than three blocks more (16 bits, D 128: one request on 32 heads, 1152 keys, 11.0 -> 7.7 us, 8 x 8 heads x 2000 19.4 -> 16.0, 4 x 4 x 65536 with
     // eight columns 88.0 -> 84.3).
     const int V = p.n * p.ctiles;
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
         total = (unsigned long long)all * p.Hkv;
         // (quotients by reciprocals: of numbers below 2^19, half a unit off the border)
         auto parts_of = [&](int size) { return (int)(((float)nb + ((float)size - 0.5f)) * (1.f / (float)size)); };
-        if (2 * V * p.Hkv <= G && total < (1u << 19)) {
+        if ((long long)V * p.Hkv <= G && total < (1u << 19)) {
             const int least = (int)(((float)(unsigned)total + ((float)G - 0.5f)) * (1.f / (float)G));
 #pragma unroll 1
             for (int k = 0; k < 4 && !part; ++k)

@@ -94,10 +94,10 @@ def test_parts_of_few_work_groups_fit_the_grid(seed):
     rng = np.random.default_rng(100 + seed)
     G = int(rng.choice([148, 296, 444]))
     V = int(rng.integers(1, 33))
-    heads = int(rng.integers(1, max(2, G // (2 * V) + 1)))
+    heads = int(rng.integers(1, max(2, G // V + 1)))
     nbs = [int(x) for x in rng.integers(1, rng.choice([3, 40, 2000]), size=V)]
     total = sum(nbs) * heads
-    if 2 * V * heads > G or total >= 1 << 19:
+    if V * heads > G or total >= 1 << 19:
         pytest.skip("not its to take")
     least = int((np.float32(total) + (np.float32(G) - np.float32(0.5))) * (np.float32(1) / np.float32(G)))
     part = next((least + k for k in range(4) if sum(_parts(nb, least + k) for nb in nbs) * heads <= G), 0)
