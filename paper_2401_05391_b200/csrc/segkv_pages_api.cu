@@ -69,10 +69,19 @@ bool many_rows(const segkv_pages* h, int n, int q_len, long long q_stride, int p
     return (double)n * h->kv_heads * ctiles * u > (double)((items + h->sm_count - 1) / h->sm_count) * r;
 }
 
+// One or two groups of 128 rows per CTA of that kernel (16 bits; 0: its own rule, made for prompts, whose items grow with their rows)?
+// Where the rows stand behind a long context all items are equally long, and what counts is rounds: a round of one takes 1.5 us for
+// 128 keys, of two 2.15.  (Whether the context is long is guessed from the table's width.)  One / two, us, 32 x 4 heads, 512 tokens, 2560 keys: 1 sequence
+// 33.2 / 45.1, 2 60.9 / 51.0, 3 86.9 / 82.3, 4 112 / 83.1; head_dim 64, 32 x 8, 54.0 / 45.8; a prompt alone, 32 x 32 x 1024, 20.3 / 24.7.
+int row_groups(const segkv_pages* h, int n, int q_len, int pack, int table_stride) {
+    if (h->bits != 16 || 2LL * q_len > (long long)table_stride * h->page_size) return 0;
+    const long long rows = (long long)q_len << pack, heads = (long long)n * (h->heads >> pack), sms = h->sm_count;
+    const long long one = (heads * ((rows + 127) / 128) + sms - 1) / sms, two = (heads * ((rows + 255) / 256) + sms - 1) / sms;
+    return two * 2.15 < one * 1.5 ? 2 : 1;
+}
+
 void free_all(segkv_pages* h) {
-    void* ptrs[] = {h->ws, h->tickets, h->err_word};
-    for (void* p : ptrs)
-        if (p) cudaFree(p);
+    if (h->ws) cudaFree(h->ws);
 }
 
 }  // namespace
@@ -111,11 +120,12 @@ int segkv_pages_create(segkv_pages_t* out, int heads, int kv_heads, int head_dim
     SEGKV_TRY(cudaGetDevice(&h->device));
     SEGKV_TRY(cudaDeviceGetAttribute(&h->sm_count, cudaDevAttrMultiProcessorCount, h->device));
     const size_t grid = (size_t)pages_sdpa_grid(*h);
-    SEGKV_TRY(cudaMalloc((void**)&h->ws, grid * 2 * pages_sdpa_slot_floats(*h) * sizeof(float)));
-    SEGKV_TRY(cudaMalloc((void**)&h->tickets, grid * sizeof(int)));
-    SEGKV_TRY(cudaMalloc((void**)&h->err_word, sizeof(int)));
-    SEGKV_TRY(cudaMemset(h->tickets, 0, grid * sizeof(int)));
-    SEGKV_TRY(cudaMemset(h->err_word, 0, sizeof(int)));
+    // one allocation: partial results, counters, error word
+    const size_t ws_bytes = grid * 2 * pages_sdpa_slot_floats(*h) * sizeof(float);
+    SEGKV_TRY(cudaMalloc((void**)&h->ws, ws_bytes + (grid + 1) * sizeof(int)));
+    h->tickets = reinterpret_cast<int*>(reinterpret_cast<char*>(h->ws) + ws_bytes);
+    h->err_word = h->tickets + grid;
+    SEGKV_TRY(cudaMemset(h->tickets, 0, (grid + 1) * sizeof(int)));
 #undef SEGKV_TRY
     if (kv_bits == 16) {
         // for the tensor-core kernel of many query rows: a copy brings the rows of one page, or of one of its tiles
@@ -188,7 +198,7 @@ int segkv_pages_sdpa(segkv_pages_t h, int n, int q_len, const void* q, long long
         a.q = q; a.out = out; a.slopes = alibi_slopes; a.err_word = h->err_word;
         a.prompt_len = q_len << pack;
         a.tm_k = &h->tm_k; a.tm_v = &h->tm_v; a.plens = nullptr; a.tm_k_src = a.tm_v_src = nullptr; a.tm_q = &tm_q;
-        a.row_groups = 0; a.pdl = h->overlap; a.wait_ns = 0; a.dbg_skip = false;
+        a.row_groups = row_groups(h, n, q_len, pack, table_stride); a.pdl = h->overlap; a.wait_ns = 0; a.dbg_skip = false;
         a.table = table; a.lens = lens; a.table_stride = table_stride; a.page_log = h->page_log; a.num_pages = h->num_pages;
         a.q_len = q_len; a.pack_log = pack; a.box_log = h->box_log;
         if (h->bits == 4) {
