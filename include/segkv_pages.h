@@ -17,7 +17,7 @@
  *     append, attention and read alike: a step raises it once and makes all its calls with it.  A length of 0 is
  *     an empty slot of a padded batch;
  *   - what only the device can see is not refused but flagged in the device error word (segkv_pages_get_error):
- *     SEGKV_DEV_BAD_PAGE: a page id outside the pool, or a length that is negative or longer than the table's row.
+ *     SEGKV_DEV_BAD_PAGE: a page id outside the pool, or a length that is negative or longer than the table's row (or than 2^31 - 4096).
  *       A token whose page is bad or whose position is behind the row is not stored; the read takes page 0 for a
  *       bad page and leaves out positions behind the row; the attention takes page 0 and clamps the length;
  *     SEGKV_DEV_BAD_POSITION: a token's position lies behind the rotation tables: it is not stored, nor its query rotated;
@@ -64,7 +64,7 @@ SEGKV_API size_t segkv_pages_bytes(int kv_heads, int head_dim, int page_size, in
 SEGKV_API int segkv_pages_create(segkv_pages_t* out, int heads, int kv_heads, int head_dim, int page_size, int num_pages,
                                  int dtype, int kv_bits, void* k_pages, void* v_pages);
 
-/* Free what the handle owns (not the pages).  Synchronises the device.  NULL is allowed. */
+/* Free what the handle owns (not the pages).  Synchronises its device, whichever is current.  NULL is allowed. */
 SEGKV_API int segkv_pages_destroy(segkv_pages_t h);
 
 /*
@@ -102,7 +102,8 @@ SEGKV_API int segkv_pages_append(segkv_pages_t h, int n, int tokens, const void*
  * rounded to the dtype first.  The work is shared out on the device by the sequences' real lengths, so a captured call follows them.
  * A value row that is not finite reaches the rows that see it; with q_len > 1 it can also reach earlier rows of the
  * same sequence, whose weight for it is zero (0 * Inf is NaN).  Rows of a page behind a sequence's end reach nothing.
- * n or q_len 0: nothing to do.  Errors: EINVAL, ECUDA.
+ * SEGKV_DEV_WAIT_LIMIT is set, and the output not written in part, if a bounded wait of the kernel for many rows runs out (never
+ * expected).  n or q_len 0: nothing to do.  Errors: EINVAL, ECUDA.
  */
 SEGKV_API int segkv_pages_sdpa(segkv_pages_t h, int n, int q_len, const void* q, long long q_stride, void* out,
                                const int32_t* table, int table_stride, const int32_t* lens, const float* alibi_slopes,

@@ -15,6 +15,8 @@ constexpr int kMaxSplits = 64;     // CTAs that may share one (request, kv head)
 constexpr int kMaxCluster = 8;     // largest portable thread-block cluster
 constexpr int kMaxTiledBeams = 16;  // beams the tiled kernel handles (16 query columns at most)
 
+constexpr long long kMaxTokens = 0x7FFFF000LL;   // longest sequence in pages: block counts and positions stay within 32 bits
+
 // {row, mask} pairs.  In the per-request list of DISTINCT response rows `row` indexes the
 // response segment's [step*rows + slot] axis; in the per-key record of a response tile in
 // shared memory it is the key's step.  `mask` has bit j set when beam j reads the row.

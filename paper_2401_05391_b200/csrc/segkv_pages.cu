@@ -65,7 +65,7 @@ __device__ __forceinline__ Place place_of(const TokenParams& p, int s, int i, in
     if (i >= nw) return r;
     const int len = __ldg(p.lens + s);
     const long long pos = (long long)len - nw + i;
-    if (len < 0 || pos >= (long long)p.table_stride << p.page_log) {
+    if (len < 0 || pos >= min((long long)p.table_stride << p.page_log, kMaxTokens)) {
         atomicOr(p.err, SEGKV_DEV_BAD_PAGE);
         return r;
     }

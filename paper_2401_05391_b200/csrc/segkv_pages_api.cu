@@ -146,8 +146,12 @@ int segkv_pages_create(segkv_pages_t* out, int heads, int kv_heads, int head_dim
 
 int segkv_pages_destroy(segkv_pages_t h) {
     if (!h) return SEGKV_OK;
+    int dev = h->device;
+    cudaGetDevice(&dev);
+    if (dev != h->device) cudaSetDevice(h->device);
     cudaDeviceSynchronize();
     free_all(h);
+    if (dev != h->device) cudaSetDevice(dev);
     delete h;
     return SEGKV_OK;
 }
@@ -230,7 +234,10 @@ int segkv_pages_set_overlap(segkv_pages_t h, int enable) {
 
 int segkv_pages_get_error(segkv_pages_t h, int* device_flags) {
     if (!h || !device_flags) return SEGKV_EINVAL;
-    cudaError_t e = cudaDeviceSynchronize();
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && dev != h->device) return SEGKV_EINVAL;
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e == cudaSuccess) e = cudaMemcpy(device_flags, h->err_word, sizeof(int), cudaMemcpyDeviceToHost);
     if (e == cudaSuccess) e = cudaMemset(h->err_word, 0, sizeof(int));
     return e == cudaSuccess ? SEGKV_OK : report_cuda(e, "segkv_pages_get_error");

@@ -60,15 +60,6 @@ cudaError_t launch_pages_sdpa(const segkv_pages& h, const PageSdpaArgs& a, cudaS
 int pages_sdpa_grid(const segkv_pages& h);                  // most CTAs of an attention launch
 size_t pages_sdpa_slot_floats(const segkv_pages& h);        // floats of one CTA's partial result
 
-// What the position and page of a token come to.
-__device__ __forceinline__ int clamped_len(int len, int most, int* err) {
-    if (len < 0 || len > most) {
-        atomicOr(err, SEGKV_DEV_BAD_PAGE);
-        return len < 0 ? 0 : most;
-    }
-    return len;
-}
-
 // launches of the library outside segkv_api.cu: errors in its manner, order on its streams
 int report_cuda(cudaError_t e, const char* what);
 void log_launch(int device, cudaStream_t st, Release rel);

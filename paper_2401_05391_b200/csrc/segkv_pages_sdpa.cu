@@ -159,7 +159,7 @@ struct Cursor {                      // a block of keys in the grid's order
 template <int NC, int KB>
 __device__ __forceinline__ void extent(const Params& p, int v, int* klen, int* nb, bool flag) {
     const int s = v / p.ctiles, ct = v - s * p.ctiles;
-    const int most = (int)min((long long)p.table_stride << p.page_log, 0x7FFFFFFFLL);
+    const int most = (int)min((long long)p.table_stride << p.page_log, kMaxTokens);
     int len = __ldg(p.lens + s);
     if (len < 0 || len > most) {
         if (flag) atomicOr(p.err, SEGKV_DEV_BAD_PAGE);

@@ -294,7 +294,7 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     // longest one, and a shorter request leaves its later items (and the tail of one) without work.  (Lengths and slopes are read
     // by plain loads: the kernel before may write them, and a read-only load need not stay behind the wait for it below.)
     auto request_len = [&](int b) -> int {
-        if constexpr (PAGED) return min(max(p.lens[b], 0), (int)min((long long)p.table_stride << p.page_log, 0x7FFFFFFFLL));
+        if constexpr (PAGED) return min(max(p.lens[b], 0), (int)min((long long)p.table_stride << p.page_log, kMaxTokens));
         return RAGGED ? p.plens[b] : p.N;
     };
     // the position of packed row r of a sequence of nb tokens (PAGED; below 0: it sees nothing); rows behind the last see what it sees

@@ -219,7 +219,8 @@ class PagedKV:
 
     def get_error(self) -> int:
         flags = _int(0)
-        _check(lib().segkv_pages_get_error(self._h, ctypes.byref(flags)), "segkv_pages_get_error")
+        with torch.cuda.device(self.device):
+            _check(lib().segkv_pages_get_error(self._h, ctypes.byref(flags)), "segkv_pages_get_error")
         return flags.value
 
     @property
