@@ -936,6 +936,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                 }
                 const int d = BITS == 16 ? 64 * r + mloc : (mloc >> 3) * (D / 8) + 8 * r + (mloc & 7);
                 if (whole) {
+                    if (lall == 0.f) a = make_float4(0.f, 0.f, 0.f, 0.f);              // a row that sees nothing: zeros, whatever the values are
                     if (there && col < p.cols) {
                         uint2 w2;
                         w2.x = M::pack(a.x * inv, a.y * inv);
@@ -1013,6 +1014,9 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                         }
                     }
                     const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                    if (sum == 0.f)
+#pragma unroll
+                        for (int r = 0; r < D / 64; ++r) acc[r] = make_float4(0.f, 0.f, 0.f, 0.f);
                     if (col < p.cols) {
                         const int row = col / p.group, hq = cur.h * p.group + (col - row * p.group);
 #pragma unroll

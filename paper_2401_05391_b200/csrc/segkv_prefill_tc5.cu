@@ -1003,7 +1003,7 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll
             for (int i = 0; i < TPR; ++i) l_run += xrow[i * kRows];
             bar_sync_n(rows_bar, 32 * TPR);
-            const float inv = PAGED && l_run == 0.f ? 0.f : 1.f / l_run;
+            const float inv = 1.f / l_run;                // (paged: 0 where a row sees nothing, which is 0 below whatever the values are)
             // NP lanes trade 16-byte pieces of their rows, so that a store instruction writes 64 (32) bytes of each of 8 (16) rows
             // instead of 16 of 32: with one row per lane the stores of an item took 3400 clocks (6500 at head_dim 256).
             constexpr int EC = DH < 32 ? DH : 32, NP = EC / 8;    // columns at a time; pieces of a row and lanes that trade
@@ -1022,7 +1022,7 @@ prefill_tc5_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 for (int i = 0; i < NP; ++i)
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
-                        v[i][u] = Mma<T>::pack(__uint_as_float(orr[8 * i + 2 * u]) * inv, __uint_as_float(orr[8 * i + 2 * u + 1]) * inv);
+                        v[i][u] = PAGED && l_run == 0.f ? 0u : Mma<T>::pack(__uint_as_float(orr[8 * i + 2 * u]) * inv, __uint_as_float(orr[8 * i + 2 * u + 1]) * inv);
 #pragma unroll
                 for (int x = 1; x < NP; x <<= 1) {                // an NP x NP transposition, an exchange per bit
                     const bool up = (lane & x) != 0;

@@ -192,6 +192,22 @@ def test_values_that_are_not_finite_stay_with_their_sequence(bits):
     c.destroy()
 
 
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("T,lens", [(3, [1, 2, 0, 7]), (200, [1, 130, 0, 450])])
+def test_rows_that_see_nothing_are_zero_whatever_the_values_are(bits, T, lens):
+    c, table, n_lens = filled(8, 2, 128, 16, lens, F16, bits, 53)
+    if bits == 16:
+        c.v_pages.fill_(math.nan)
+        c.v_pages[..., ::3] = math.inf
+    else:
+        pg.split4(c.v_pages, 16, 128, F16)[1].fill_(math.nan)
+    out = c.sdpa(randn(len(lens), T, 8, 128, dtype=F16, g=gen(54)), table, n_lens)
+    for b, x in enumerate(lens):
+        assert torch.equal(out[b, :max(T - x, 0)], torch.zeros_like(out[b, :max(T - x, 0)]))
+        assert not torch.isfinite(out[b, max(T - x, 0):]).any()
+    c.destroy()
+
+
 def test_query_rows_of_a_packed_projection():
     c, table, n_lens = filled(8, 2, 64, 16, [33, 90], F16, 16, 61)
     x = randn(2, 3, 8 + 4, 64, dtype=F16, g=gen(62))
