@@ -102,6 +102,7 @@ SEGKV_API int segkv_pages_append(segkv_pages_t h, int n, int tokens, const void*
  * rounded to the dtype first.  The work is shared out on the device by the sequences' real lengths, so a captured call follows them.
  * A value row that is not finite reaches the rows that see it; with q_len > 1 it can also reach earlier rows of the
  * same sequence, whose weight for it is zero (0 * Inf is NaN).  Rows of a page behind a sequence's end reach nothing.
+ * Pieces of prompts (many query rows) ask for scores below 2^24 in size; what a sum in fp32 still tells apart ends there.
  * SEGKV_DEV_WAIT_LIMIT is set, and the output not written in part, if a bounded wait of the kernel for many rows runs out (never
  * expected).  n or q_len 0: nothing to do.  Errors: EINVAL, ECUDA.
  */

@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
     float qs[2];                                              // NARROW: this lane's group's sums
     int lim[NT][2];                                           // keys below it are seen
     float scale2[NT][2], slope[NT][2];                        // of a raw score; of a key's distance, in raw scores
-    float mref[NT][2], thr[NT][2], base[NT][2], lsum[NT][2];  // reference, what moves it, its exponent; sum of weights
+    float mref[NT][2], thr[NT][2], base[NT][2], lsum[NT][2];  // reference, what moves it, what is taken off a score; sum of weights
     float o[NT][MT][4];
     float zo[BITS == 4 ? NT : 1][4];
     int vexp;                                                 // 4 bits: exponent that the values' scales are taken relative to
@@ -460,8 +460,9 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                 }
                 big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
                 big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-                // the column by a power of two: its largest value between 1 and 2 (values 2^-24 of it lose bits; 0, Inf and NaN stay so)
-                const int ex = min(max(__float_as_int(big) >> 23, 1), 253);
+                // the column by a power of two: its largest value between 1 and 2 (values 2^-24 of it lose bits; 0, Inf and NaN stay so).
+                // Beside a bias not below 2^-90, or a key's distance in such scores would leave fp32.
+                const int ex = min(max(__float_as_int(big) >> 23, BIAS ? 127 - 90 : 1), 253);
                 const float down = big > 0.f ? __int_as_float((254 - ex) << 23) : 1.f;
                 unit = big > 0.f ? __int_as_float(ex << 23) : 1.f;
                 float sum[4] = {0.f, 0.f, 0.f, 0.f};
@@ -684,7 +685,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                             const float al = mref[nt][e] == -INFINITY ? 1.f : exp2f((mref[nt][e] - mx) * scale2[nt][e]);
                             mref[nt][e] = mx;
                             thr[nt][e] = mx + kSlack / scale2[nt][e];
-                            base[nt][e] = mx == -INFINITY ? 0.f : mx * scale2[nt][e] - kUp;
+                            base[nt][e] = mx == -INFINITY ? 0.f : mx;
                             lsum[nt][e] *= al;
 #pragma unroll
                             for (int m = 0; m < MT; ++m) {
@@ -698,14 +699,16 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                         }
                 }
                 // ---- weights and values -------------------------------------------------------------------------------------------
+                // (the difference first: scale * score - rounded(scale * reference) in one operation is off by the rounding, which is more
+                // than an exponent holds where scores pass 2^31)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
 #pragma unroll
                         for (int u = 0; u < SUB; ++u) {
-                            c[u][nt][e] = exp2f(fmaf(c[u][nt][e], scale2[nt][e], -base[nt][e]));
-                            c[u][nt][e + 2] = exp2f(fmaf(c[u][nt][e + 2], scale2[nt][e], -base[nt][e]));
+                            c[u][nt][e] = exp2f(fmaf(c[u][nt][e] - base[nt][e], scale2[nt][e], kUp));
+                            c[u][nt][e + 2] = exp2f(fmaf(c[u][nt][e + 2] - base[nt][e], scale2[nt][e], kUp));
                             lsum[nt][e] += c[u][nt][e] + c[u][nt][e + 2];
                         }
                     }
@@ -877,7 +880,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                 l += __shfl_xor_sync(0xffffffffu, l, 16);
                 if (g == 0 && (!NARROW || t == 0)) {
                     float* ml = s_ml + (warp * NC + (NARROW ? e : nt * 8 + 2 * t + e)) * 2;
-                    ml[0] = mref[nt][e] == -INFINITY ? -INFINITY : mref[nt][e] * scale2[nt][e];
+                    ml[0] = mref[nt][e] == -INFINITY ? -INFINITY : __fmul_rn(mref[nt][e], scale2[nt][e]);
                     ml[1] = l;
                 }
             }
@@ -903,7 +906,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                 for (int w = 0; w < kWarps; ++w) top[e] = fmaxf(top[e], s_ml[(w * NC + (NARROW ? e : nt * 8 + 2 * t + e)) * 2]);
             float f[2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) f[e] = mref[nt][e] == -INFINITY ? 1.f : exp2f(mref[nt][e] * scale2[nt][e] - top[e]);     // (no weight: zeros, or NaN)
+            for (int e = 0; e < 2; ++e) f[e] = mref[nt][e] == -INFINITY ? 1.f : exp2f(__fmul_rn(mref[nt][e], scale2[nt][e]) - top[e]);     // (no weight: zeros, or NaN)
             float mtop = -INFINITY, lall = 0.f;
             const int lcol = NARROW ? mcol & 1 : nt * 8 + mcol;       // (NARROW: columns 2 to 7 are nobody's)
             const bool there = !NARROW || mcol < 2;

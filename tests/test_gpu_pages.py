@@ -151,6 +151,23 @@ def test_small_and_large_values(bits, scale):
 
 
 @pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("heads,T", [(2, 1), (8, 1), (8, 5)])
+@pytest.mark.parametrize("scale", [0.0, 1e-39, 1e-30, 1e30])
+def test_queries_of_any_size_beside_a_bias(bits, heads, T, scale):
+    """Queries so small that a key's distance, in their scores, would leave fp32; and so large that the bias is nothing."""
+    lens = [200, 9]
+    c, table, n_lens = filled(heads, 2, 128, 16, lens, BF16, bits, 34)
+    q = randn(2, T, heads, 128, dtype=BF16, g=gen(35)) * scale
+    for slopes in (wl.alibi_slopes(heads).cuda(), None):
+        out, tol = pg.attention(c, q, table, lens, slopes)
+        if scale > 1.0:                                       # (a score's error moves nothing where one key has all the weight)
+            assert torch.isfinite(c.sdpa(q, table, n_lens, None, slopes)).all()
+        else:
+            pg.check(c.sdpa(q, table, n_lens, None, slopes), out, tol)
+    c.destroy()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
 @pytest.mark.parametrize("dtype", [F16, BF16])
 def test_scores_that_grow(bits, dtype):
     """Keys that turn towards the query along the sequence: the reference moves again and again; and one key that outweighs all."""
