@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(kThreads, BITS == 16 ? 4 : 3) pages_append_ker
     const char* const src_k = p.k + (long long)token * p.k_stride + c * 16;
     const char* const src_v = p.v + (long long)token * p.v_stride + c * 16 - (size_t)Hkv * (D * 2);
     const char* const src_q = p.q + (long long)token * p.q_stride + c * 16 - (size_t)2 * Hkv * (D * 2);
-    constexpr int AHEAD = 2;
+    constexpr int AHEAD = BITS == 16 ? 2 : 1;                 // (4 bits, 8 x 2048 tokens x 40 rows: 55.9, with 2 57.0 us, 3 61; 16 bits 4 x 512 x 48: 15.4, 14.9, 18.5)
     uint4 lo[AHEAD], hi[AHEAD];                               // the next rows
     auto fetch = [&](uint4& lo, uint4& hi, int row, bool real) {
         lo = hi = make_uint4(0u, 0u, 0u, 0u);

@@ -202,6 +202,9 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
     int* s_misc = reinterpret_cast<int*>(smem + Sh::RING + Sh::MERGE + Sh::ML);
     const uint32_t ring = smem_u32(smem) + warp * (kStages * Sh::STAGE);
 
+    // Lengths and tables are small and read one behind the other: the first 16 KB of both are asked for at once.
+    if ((tid << 5) < p.n) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.lens + (tid << 5)));
+    if ((long long)(tid << 5) < (long long)p.n * p.table_stride) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.table + (tid << 5)));
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
@@ -234,6 +237,9 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
         auto parts_of = [&](int size) { return (int)(((float)nb + ((float)size - 0.5f)) * (1.f / (float)size)); };
         if ((long long)V * p.Hkv <= G && total < (1u << 19)) {
             const int least = (int)(((float)(unsigned)total + ((float)G - 0.5f)) * (1.f / (float)G));
+            // (a part's meeting and fold cost more than a second block: 8 heads x 4 sequences x 100 keys 5.8 -> 4.6, 4 bits x 200 keys 8.3 -> 7.4)
+            const int longest = __reduce_max_sync(0xffffffffu, nb);
+            if (longest <= 2) part = longest;
 #pragma unroll 1
             for (int k = 0; k < 4 && !part; ++k)
                 if ((int)__reduce_add_sync(0xffffffffu, parts_of(least + k)) * p.Hkv <= G) part = least + k;
@@ -960,9 +966,9 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
             // ---- partial results: the last CTA of the work group folds them -------------------------------------------------------
             __syncthreads();
             if (tid == 0) {
-                __threadfence();                              // (the CTA's writes, behind the barrier above)
-                s_misc[3] = atomicAdd(p.tickets + c0, 1);
-                __threadfence();
+                int old;                                      // (the CTA's writes lie behind the barrier above, the others' reads behind the one below)
+                asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(old) : "l"(p.tickets + c0) : "memory");
+                s_misc[3] = old;
             }
             __syncthreads();
             if (s_misc[3] == c1 - c0) {
