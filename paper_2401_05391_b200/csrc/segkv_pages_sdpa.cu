@@ -59,29 +59,13 @@ template <> struct Num<__nv_bfloat16> {
 };
 
 // ---- 4-bit rows: codes as fp16, whatever the dtype ----------------------------------------------------------------------------
-// Two codes of a word, in bits 0-3 and 16-19, become fp16 numbers by or-ing them into 1024 (whose last place is 1); codes in bits 4-7 and
-// 20-23 count 16.  An fp16 product takes them exactly, so the queries (scaled by a power of two per column) and the weights are
-// fp16 for a bf16 cache too: 11 bits instead of 8, and half the shifts.
-constexpr uint32_t kMagic = 0x64006400u;
+// Two codes of a word, in bits 0-3 and 16-19, are fp16 numbers as they stand: subnormal ones, c 2^-24, which a product takes exactly;
+// codes in bits 4-7 and 20-23 are 16 c 2^-24.  One instruction for two codes, no conversion.  So the queries (lifted by a power of two per column)
+// and the weights are fp16 for a bf16 cache too: 11 bits instead of 8, and half the shifts.  The 8 that a code has too much is
+// taken off by the group's sums of queries or weights.
 constexpr float kLift4 = 6.f;
-// (w & mask) | magic in one instruction
-__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask) {
-    uint32_t r;
-    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(kMagic));
-    return r;
-}
-__device__ __forceinline__ uint32_t codes_lo(uint32_t w) { return and_or(w, 0x000F000Fu); }          // 1024 + c
-__device__ __forceinline__ uint32_t codes_hi(uint32_t w) { return and_or(w, 0x00F000F0u); }          // 1024 + 16 c
-__device__ __forceinline__ uint32_t centred_lo(uint32_t w) {                                         // c - 8
-    const uint32_t x = codes_lo(w), k = 0x64086408u;                                                 // 1032
-    const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&k));
-    return *reinterpret_cast<const uint32_t*>(&r);
-}
-__device__ __forceinline__ uint32_t centred_hi(uint32_t w) {                                         // (1024 + 16 c) / 16 - 72
-    const uint32_t x = codes_hi(w), m = 0x2C002C00u, k = 0xD480D480u;
-    const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&m), *reinterpret_cast<const __half2*>(&k));
-    return *reinterpret_cast<const uint32_t*>(&r);
-}
+__device__ __forceinline__ uint32_t codes_lo(uint32_t w) { return w & 0x000F000Fu; }
+__device__ __forceinline__ uint32_t codes_hi(uint32_t w) { return w & 0x00F000F0u; }
 __device__ __forceinline__ void mma_h(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1, float c2, float c3) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
@@ -417,14 +401,13 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
     constexpr float kScale2 = D == 64 ? kLog2e * 0.125f : D == 128 ? kLog2e * 0.08838834764831845f : kLog2e * 0.0625f;
     constexpr float kUp = BITS == 4 ? kLift4 : N::kLift;      // weights are 2^kUp times what they are
     uint32_t qf[NT][QJ][2];
-    float cinit[BITS == 4 ? NT : 1][4][2];                    // 4 bits: what the magic number adds to a group's sum, negated
-    uint32_t qsum[BITS == 4 ? NT : 1];                        // 4 bits: the groups' sums of q, in two parts (B operand)
+    uint32_t qsum[BITS == 4 ? NT : 1][2];                     // 4 bits: the groups' sums of q, in two parts, and -8 times them (B operand)
     float qs[2];                                              // NARROW: this lane's group's sums
     int lim[NT][2];                                           // keys below it are seen
     float scale2[NT][2], slope[NT][2];                        // of a raw score; of a key's distance, in raw scores
     float mref[NT][2], thr[NT][2], base[NT][2], lsum[NT][2];  // reference, what moves it, what is taken off a score; sum of weights
     float o[NT][MT][4];
-    float zo[BITS == 4 ? NT : 1][4];
+    float zo[BITS == 4 ? NT : 1][4], zc[BITS == 4 ? NT : 1][4];   // 4 bits: the groups' sums of weights times zero points; of weights times scales, times -8
     int vexp;                                                 // 4 bits: exponent that the values' scales are taken relative to
 
     unsigned long long x = x0;
@@ -466,11 +449,12 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                 }
                 big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
                 big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-                // the column by a power of two: its largest value between 1 and 2 (values 2^-24 of it lose bits; 0, Inf and NaN stay so).
-                // Beside a bias not below 2^-90, or a key's distance in such scores would leave fp32.
-                const int ex = min(max(__float_as_int(big) >> 23, BIAS ? 127 - 90 : 1), 253);
-                const float down = big > 0.f ? __int_as_float((254 - ex) << 23) : 1.f;
-                unit = big > 0.f ? __int_as_float(ex << 23) : 1.f;
+                // the column by 2^-d: its largest value between 2^14 and 2^15 (values 2^-38 of it are lost; 0, Inf and NaN stay so).  Beside a
+                // bias not by more than 2^90, or a key's distance in such scores would leave fp32; and what undoes it (with the codes'
+                // 2^24) stays in fp32: queries above 2^116 would need keys below 2^-100 to notice.
+                const int d = max((__float_as_int(big) >> 23) - 141, BIAS ? -90 : -126);
+                const float down = __int_as_float((127 - d) << 23);
+                unit = __int_as_float((127 + min(d + 24, 126)) << 23);
                 float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
@@ -492,24 +476,19 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                 for (int j = 0; j < 4; ++j) {
                     sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 1);
                     sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 2);
-                    const float off = sum[j] * (j & 1 ? -(1024.f + 128.f) : -1032.f);
-                    if (!NARROW)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) cinit[nt][j][e] = __shfl_sync(0xffffffffu, off, (2 * t + e) * 4);
-                    if (j & 1) sum[j] *= 16.f;
+                    sum[j] *= j & 1 ? 0x1p-20f : 0x1p-24f;    // (in the products' units)
                 }
                 if constexpr (NARROW) {                       // this lane's group is t: of columns 0 and 1, from lanes that have them
                     const float own = t & 2 ? (t & 1 ? sum[3] : sum[2]) : (t & 1 ? sum[1] : sum[0]);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        qs[e] = __shfl_sync(0xffffffffu, own, e * 4 + t);
-                        cinit[0][0][e] = qs[e] * (t & 1 ? -72.f : -1032.f);
-                    }
+                    for (int e = 0; e < 2; ++e) qs[e] = __shfl_sync(0xffffffffu, own, e * 4 + t);
                 } else {
                     const float a = t & 1 ? sum[2] : sum[0], b = t & 1 ? sum[3] : sum[1];
                     const uint32_t hi = M::pack(a, b);
                     const float2 hf = M::unpack(hi);
-                    qsum[nt] = t < 2 ? hi : M::pack(a - hf.x, b - hf.y);
+                    qsum[nt][0] = t < 2 ? hi : M::pack(a - hf.x, b - hf.y);
+                    const float2 both = M::unpack(qsum[nt][0]);
+                    qsum[nt][1] = M::pack(-8.f * both.x, -8.f * both.y);
                 }
             }
 #pragma unroll
@@ -529,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                 for (int e = 0; e < 4; ++e) o[nt][m][e] = 0.f;
             if (BITS == 4)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) zo[nt][e] = 0.f;
+                for (int e = 0; e < 4; ++e) zo[nt][e] = zc[nt][e] = 0.f;
         }
         const int free_to = pos0 + first_row + 1;             // keys below it are seen by every row of the tile
         vexp = 0;
@@ -603,7 +582,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                                     }
                                     const uint32_t* b = qf[0][j * (W / 2) + w2];
                                     float (&d)[4] = acc[j & 1];
-                                    if (w2 == 0 && j == 0) mma_h(d, a, b[0], b[1], cinit[0][0][0], cinit[0][0][1], cinit[0][0][0], cinit[0][0][1]);
+                                    if (w2 == 0 && j == 0) mma_h(d, a, b[0], b[1], -8.f * qs[0], -8.f * qs[1], -8.f * qs[0], -8.f * qs[1]);
                                     else if (w2 == 0 && j == 1) mma_h(d, a, b[0], b[1], 0.f, 0.f, 0.f, 0.f);
                                     else mma_h(d, a, b[0], b[1], d[0], d[1], d[2], d[3]);
                                 }
@@ -618,11 +597,15 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                         const uint2 sl = lds64(sc), sh = lds64(sc + 128);
                         const float2 sl0 = M::unpack(sl.x), sl1 = M::unpack(sl.y), sh0 = M::unpack(sh.x), sh1 = M::unpack(sh.y);
                         const float fl[4] = {sl0.x, sl0.y, sl1.x, sl1.y}, fh[4] = {sh0.x, sh0.y, sh1.x, sh1.y};
-                        // zero points: sum over groups of z * (sum of q in the group)
-                        const uint32_t za = lds32(sc + 8 + (t & 1) * 4), zb = lds32(sc + 128 + 8 + (t & 1) * 4);
+                        // sum over groups of (z - 8 s) * (sum of q in the group)
+                        const uint32_t za[4] = {lds32(sc + 8 + (t & 1) * 4), lds32(sc + 128 + 8 + (t & 1) * 4), t & 1 ? sl.y : sl.x, t & 1 ? sh.y : sh.x};
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) N::mma8(c[u][nt], za, zb, qsum[nt]);
-                        // codes, group by group; the magic's share is taken off by the start value
+                        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) c[u][nt][e] = 0.f;
+                            M::run(c[u][nt], za, qsum[nt][0], qsum[nt][1]);
+                        }
+                        // codes, group by group
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             float acc[NT][4];
@@ -637,7 +620,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt) {
                                     const uint32_t* b = qf[nt][j * (W / 2) + w2];
-                                    if (w2 == 0) mma_h(acc[nt], a, b[0], b[1], cinit[nt][j][0], cinit[nt][j][1], cinit[nt][j][0], cinit[nt][j][1]);
+                                    if (w2 == 0) mma_h(acc[nt], a, b[0], b[1], 0.f, 0.f, 0.f, 0.f);
                                     else mma_h(acc[nt], a, b[0], b[1], acc[nt][0], acc[nt][1], acc[nt][2], acc[nt][3]);
                                 }
                             }
@@ -699,8 +682,8 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                                 o[nt][m][e + 2] *= al;
                             }
                             if (BITS == 4) {
-                                zo[nt][e] *= al;
-                                zo[nt][e + 2] *= al;
+                                zo[nt][e] *= al;              // (rows 0 to 3 are all that counts)
+                                zc[nt][e] *= al;
                             }
                         }
                 }
@@ -767,9 +750,11 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                                for (int m = 0; m < MT; ++m)
+                                for (int e = 0; e < 4; ++e) {
+                                    zc[nt][e] *= down;
 #pragma unroll
-                                    for (int e = 0; e < 4; ++e) o[nt][m][e] *= down;
+                                    for (int m = 0; m < MT; ++m) o[nt][m][e] *= down;
+                                }
                             vexp = top;
                         }
                     }
@@ -785,6 +770,8 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                             pf[0][0][1] = movmatrix_trans(Mma<__half>::pack(c[u][0][2] * b, c[u][0][3] * b));
                             zo[0][0] = fmaf(c[u][0][0], zz.x, fmaf(c[u][0][2], zz.y, zo[0][0]));
                             zo[0][1] = fmaf(c[u][0][1], zz.x, fmaf(c[u][0][3], zz.y, zo[0][1]));
+                            const uint32_t a8[4] = {0xC800C800u, 0u, 0xC800C800u, 0u};        // -8 on rows 0 to 7
+                            mma_h(zc[0], a8, pf[0][0][0], pf[0][0][1], zc[0][0], zc[0][1], zc[0][2], zc[0][3]);
                         } else {
                         const float2 sl0 = M::unpack(sl[u].x), sl1 = M::unpack(sl[u].y), sh0 = M::unpack(sh[u].x), sh1 = M::unpack(sh[u].y);
                         const float fl[4] = {sl0.x * unit, sl0.y * unit, sl1.x * unit, sl1.y * unit};
@@ -796,6 +783,12 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                                 pf[nt][j][0] = movmatrix_trans(Mma<__half>::pack(c[u][nt][0] * fl[j], c[u][nt][1] * fl[j]));
                                 pf[nt][j][1] = movmatrix_trans(Mma<__half>::pack(c[u][nt][2] * fh[j], c[u][nt][3] * fh[j]));
                             }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {         // row j: -8 for group j
+                            const uint32_t a8[4] = {g == j ? 0xC800C800u : 0u, 0u, g == j ? 0xC800C800u : 0u, 0u};
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) mma_h(zc[nt], a8, pf[nt][j][0], pf[nt][j][1], zc[nt][0], zc[nt][1], zc[nt][2], zc[nt][3]);
+                        }
                         // zero points: rows 0-3 of one more product are the groups'
                         {
                             uint32_t a[4] = {0u, 0u, 0u, 0u};
@@ -835,7 +828,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) {
                                     if (j == 2) r[i] >>= 8;
-                                    a[i] = j & 1 ? centred_hi(r[i]) : centred_lo(r[i]);
+                                    a[i] = j & 1 ? codes_hi(r[i]) : codes_lo(r[i]);
                                 }
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt) {
@@ -856,7 +849,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
             const float up = __int_as_float((127 + vexp - N::kExpBias) << 23);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                float zg[4][2];
+                float zg[4][2], z8[4][2];
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -866,14 +859,16 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                             z += __shfl_xor_sync(0xffffffffu, z, 4);
                             z += __shfl_xor_sync(0xffffffffu, z, 8);
                             zg[j][e] = z + __shfl_xor_sync(0xffffffffu, z, 16);
+                            z8[j][e] = zc[0][e];
                         } else {
                             zg[j][e] = __shfl_sync(0xffffffffu, zo[nt][e], j * 4 + t);
+                            z8[j][e] = __shfl_sync(0xffffffffu, zc[nt][e], j * 4 + t);
                         }
                     }
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[nt][m][e] = fmaf(o[nt][m][e], up, zg[m & 3][e & 1]);
+                    for (int e = 0; e < 4; ++e) o[nt][m][e] = fmaf(fmaf(o[nt][m][e], m & 1 ? 0x1p20f : 0x1p24f, z8[m & 3][e & 1]), up, zg[m & 3][e & 1]);
             }
         }
 #pragma unroll
