@@ -142,6 +142,8 @@ __device__ __forceinline__ void quantise(const uint32_t (&w)[8], uint32_t (&code
     }
     uint32_t sw[2], zw[2];
     float s[4], z[4], inv[4];
+    uint32_t dead = 0u;                                       // codes of groups whose scale is 0 or NaN: 8
+    bool tiny = false;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const float2 lo = H::up(mn[j]), hi = H::up(mx[j]);
@@ -159,36 +161,42 @@ __device__ __forceinline__ void quantise(const uint32_t (&w)[8], uint32_t (&code
         const float2 x = H::up(sw[j]), y = H::up(zw[j]);
         s[2 * j] = x.x; s[2 * j + 1] = x.y;
         z[2 * j] = y.x; z[2 * j + 1] = y.y;
-        inv[2 * j] = x.x > 0.f ? 1.f / x.x : 0.f;             // (0 and NaN: every code is 8)
-        inv[2 * j + 1] = x.y > 0.f ? 1.f / x.y : 0.f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const float sc = s[2 * j + u];
+            inv[2 * j + u] = __frcp_rn(sc);
+            if (!(sc > 0.f)) dead |= 0x000F000Fu << (4 * (2 * j + u));
+            tiny |= sc > 0.f && sc < 0x1p-100f;
+        }
     }
-    // code = rint((x - z)/s) + 8, clamped.  The quotient is a product with the reciprocal, good to 2^-21 of it; adding 1.5 * 2^23 rounds
-    // it (ties to even) and leaves the code in the low bits.  Where it stands within 2e-5 of a tie the row's words are done again
-    // by division.  (Far outside the range, where z's rounding is all there is, the quotient may be large: the clamp is before the bits.)
+    // code = rint((x - z)/s) + 8, clamped.  Quotient: y times the rounded reciprocal, and one step with the exact remainder y - q s.  The
+    // step leaves 2^-45 of the quotient, and one of y (24 bits) by s (11 at most) is never that near to the middle of two fp32
+    // numbers without lying on it, so this is the quotient as a division rounds it.  Adding 1.5 * 2^23 rounds it to a whole number (ties to even) and
+    // leaves the code in the low bits.  A remainder below 2^-126 would be lost: scales below 2^-100 are divided by.
     constexpr float kRound = 12582912.f;
-    bool near = false;
     code[0] = code[1] = 0u;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
         const float2 f = H::up(w[e >> 1]);
-        const float i = inv[e & 3], y = i > 0.f ? __fsub_rn(e & 1 ? f.y : f.x, z[e & 3]) : 0.f;
-        const float r = fmaf(y, i, kRound + 8.f);
-        near |= fabsf(fmaf(y, i, kRound + 8.f - r)) > 0.49998f;
+        const int j = e & 3;
+        const float y = __fsub_rn(e & 1 ? f.y : f.x, z[j]), q = __fmul_rn(y, inv[j]);
+        const float r = __fadd_rn(__fmaf_rn(__fmaf_rn(-q, s[j], y), inv[j], q), kRound + 8.f);
         code[e >> 3] += __float_as_uint(fminf(fmaxf(r, kRound), kRound + 15.f)) << (4 * (e & 7));
     }
-    if (near) {
+    if (tiny) {
         code[0] = code[1] = 0u;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const float2 f = H::up(w[e >> 1]);
-            const float i = inv[e & 3], y = __fsub_rn(e & 1 ? f.y : f.x, z[e & 3]);
-            const float r = i > 0.f ? __fdiv_rn(y, s[e & 3]) : 0.f;
+            const float r = __fdiv_rn(__fsub_rn(e & 1 ? f.y : f.x, z[e & 3]), s[e & 3]);
             code[e >> 3] += __float_as_uint(fminf(fmaxf(r + (kRound + 8.f), kRound), kRound + 15.f)) << (4 * (e & 7));
         }
     }
     constexpr uint32_t kBits = 0x4B400000u;                   // of kRound: what the eight sums have too much (the rest has left at the top)
     code[0] -= kBits + (kBits << 4) + (kBits << 8);
     code[1] -= kBits + (kBits << 4) + (kBits << 8);
+    code[0] = (code[0] & ~dead) | (0x88888888u & dead);
+    code[1] = (code[1] & ~dead) | (0x88888888u & dead);
     *scales = make_uint4(sw[0], sw[1], zw[0], zw[1]);
 }
 
@@ -213,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, BITS == 16 ? 4 : 3) pages_append_ker
     const char* const src_k = p.k + (long long)token * p.k_stride + c * 16;
     const char* const src_v = p.v + (long long)token * p.v_stride + c * 16 - (size_t)Hkv * (D * 2);
     const char* const src_q = p.q + (long long)token * p.q_stride + c * 16 - (size_t)2 * Hkv * (D * 2);
-    constexpr int AHEAD = BITS == 16 ? 2 : 1;                 // (4 bits, 8 x 2048 tokens x 40 rows: 55.9, with 2 57.0 us, 3 61; 16 bits 4 x 512 x 48: 15.4, 14.9, 18.5)
+    constexpr int AHEAD = BITS == 16 ? 2 : 1;                 // (4 bits, 8 x 2048 tokens x 40 rows with the read: 68.0, with 2 69.1 us, 3 73.5; 16 bits 4 x 512 x 48: 15.4, 14.9, 18.5)
     uint4 lo[AHEAD], hi[AHEAD];                               // the next rows
     auto fetch = [&](uint4& lo, uint4& hi, int row, bool real) {
         lo = hi = make_uint4(0u, 0u, 0u, 0u);
