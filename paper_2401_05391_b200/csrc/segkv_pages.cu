@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, BITS == 16 ? 4 : 3) pages_append_ker
     const char* const src_k = p.k + (long long)token * p.k_stride + c * 16;
     const char* const src_v = p.v + (long long)token * p.v_stride + c * 16 - (size_t)Hkv * (D * 2);
     const char* const src_q = p.q + (long long)token * p.q_stride + c * 16 - (size_t)2 * Hkv * (D * 2);
-    constexpr int AHEAD = BITS == 16 ? 2 : 1;                 // (4 bits, 8 x 2048 tokens x 40 rows with the read: 68.0, with 2 69.1 us, 3 73.5; 16 bits 4 x 512 x 48: 15.4, 14.9, 18.5)
+    constexpr int AHEAD = BITS == 16 ? 2 : 1;                 // (4 bits, 8 x 2048 tokens x 40 rows with the read: 68.0, with 2 69.1 us, 3 73.5; 16 bits, 4 x 512 x 48 rows: 1 15.4, 2 14.9, 3 18.5)
     uint4 lo[AHEAD], hi[AHEAD];                               // the next rows
     auto fetch = [&](uint4& lo, uint4& hi, int row, bool real) {
         lo = hi = make_uint4(0u, 0u, 0u, 0u);
@@ -234,20 +234,36 @@ __global__ void __launch_bounds__(kThreads, BITS == 16 ? 4 : 3) pages_append_ker
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) fetch(lo[i], hi[i], row0 + rl + i * rs, token < p.t.tokens);      // (before it is known whether it is padding, which is there to be read)
     find_places(p.t, s_place, STYLE ? p.positions : 0x7FFFFFFF, false);
+    float co[8], si[8];
+    if (STYLE != 0 && token < p.t.tokens) {                   // angles: by the length alone, while the page is looked up
+        const int s = token / p.t.T;
+        int nw = p.t.new_lens ? __ldg(p.t.new_lens + s) : p.t.T;
+        nw = nw < 0 ? 0 : nw > p.t.T ? p.t.T : nw;
+        const long long pos = (long long)__ldg(p.t.lens + s) - nw + (token - s * p.t.T);
+        if (pos >= 0 && pos < p.positions) {
+            const float* cs = p.cos + (size_t)pos * (D / 2);
+            const float* sn = p.sin + (size_t)pos * (D / 2);
+            // interleaved: pairs 4c .. of the lower half, then of the upper
+            const int i0 = STYLE == SEGKV_ROPE_HALF ? c * 8 : c * 4, i1 = STYLE == SEGKV_ROPE_HALF ? c * 8 + 4 : c * 4 + D / 4;
+            if (((reinterpret_cast<uintptr_t>(p.cos) | reinterpret_cast<uintptr_t>(p.sin)) & 15) == 0) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const float4 a = __ldg(reinterpret_cast<const float4*>(cs + (u ? i1 : i0))), b = __ldg(reinterpret_cast<const float4*>(sn + (u ? i1 : i0)));
+                    co[4 * u] = a.x; co[4 * u + 1] = a.y; co[4 * u + 2] = a.z; co[4 * u + 3] = a.w;
+                    si[4 * u] = b.x; si[4 * u + 1] = b.y; si[4 * u + 2] = b.z; si[4 * u + 3] = b.w;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    co[e] = __ldg(cs + (e < 4 ? i0 + e : i1 + e - 4));
+                    si[e] = __ldg(sn + (e < 4 ? i0 + e : i1 + e - 4));
+                }
+            }
+        }
+    }
     __syncthreads();
     const Place at = s_place[tl];
     const bool real = at.row >= 0;
-    float co[8], si[8];
-    if (STYLE != 0 && real) {
-        const float* cs = p.cos + (size_t)at.pos * (D / 2);
-        const float* sn = p.sin + (size_t)at.pos * (D / 2);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {                         // interleaved: pairs 4c .. of the lower half, then of the upper
-            const int i = STYLE == SEGKV_ROPE_HALF ? c * 8 + e : c * 4 + (e & 3) + (e >> 2) * (D / 4);
-            co[e] = __ldg(cs + i);
-            si[e] = __ldg(sn + i);
-        }
-    }
     char* const dst_q = p.q_out + ((size_t)token * p.H) * (D * 2) + c * 16 - (size_t)2 * Hkv * (D * 2);
     const int ps = 1 << p.t.page_log, in_page = (int)(at.row & (ps - 1));
     const size_t block = (size_t)ps * (D / 2 + 16);                                    // 4 bits: bytes of one head's rows in a page

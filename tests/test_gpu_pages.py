@@ -340,6 +340,48 @@ def test_append_bit_for_bit(shape, dtype, bits, style):
     c.destroy()
 
 
+@pytest.mark.parametrize("style", ["half", "interleaved"])
+@pytest.mark.parametrize("D", [64, 256])
+def test_rotation_tables_of_any_alignment(D, style):
+    table, lens = torch.tensor([[1, 0], [2, -1]], dtype=torch.int32, device="cuda"), torch.tensor([20, 9], dtype=torch.int32, device="cuda")
+    q, k, v = packed(2, 9, 4, 2, D, F16, 81)
+    tables = [x.cuda() for x in wl.rope_tables(20, D)]
+    shifted = []
+    for x in tables:
+        flat = torch.empty(x.numel() + 1, device="cuda")[1:]
+        shifted.append(flat.view_as(x).copy_(x))
+    got = []
+    for cos, sin in (tables, shifted, (tables[0], shifted[1])):
+        c = PagedKV(4, 2, D, 16, 3, F16, 16)
+        c.k_pages.zero_()
+        got.append((c.append(k, v, table, lens, q=q, rope_cos=cos, rope_sin=sin, style=style), c.k_pages.clone()))
+        c.destroy()
+    for q_out, pages in got[1:]:
+        assert torch.equal(q_out, got[0][0]) and torch.equal(pages, got[0][1])
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("scale", [2.0 ** -20, 1.0, 2.0 ** 9])
+def test_codes_of_values_halfway_between_two(dtype, scale):
+    """Values on, and one unit beside, the middle between two codes: the rounded quotient decides, ties to even."""
+    n, D, ps = 64, 128, 64
+    rng = np.random.default_rng(17)
+    c = PagedKV(4, 4, D, ps, n, dtype, 4)
+    step = torch.from_numpy(rng.integers(128, 256, (n * ps, 1, 1, 4)) * scale / 64.0)
+    k = torch.from_numpy(rng.integers(-8, 8, (n * ps, 4, D // 4, 4)) + 0.5 * rng.integers(0, 2, (n * ps, 4, D // 4, 4)))
+    k[:, :, 0], k[:, :, 1] = -8, 7                             # (the whole range, so that the scale is the step or its neighbour)
+    x = (step * k + torch.from_numpy(rng.integers(-40, 40, (n * ps, 4, 1, 4))) * step / 8).to(dtype).flatten(-2)
+    side = torch.from_numpy(rng.integers(-1, 2, x.shape)).to(torch.int16)
+    x = (x.view(torch.int16) + torch.where(x == 0, torch.zeros_like(side), side)).view(dtype).cuda().view(n, ps, 4, D)
+    table = torch.arange(n, dtype=torch.int32, device="cuda").view(n, 1)
+    c.append(x, x, table, torch.full((n,), ps, dtype=torch.int32, device="cuda"))
+    codes, scales = pg.split4(c.k_pages, ps, D, dtype)
+    cd, s, z = pg.codes_of(x.transpose(1, 2), dtype)
+    assert torch.equal(scales, torch.cat([s, z], -1)) and torch.equal(codes, cd[..., 0::2] | (cd[..., 1::2] << 4))
+    assert torch.equal(c.k_pages, c.v_pages) and c.get_error() == 0
+    c.destroy()
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16])
 def test_four_bit_rows_at_the_edges(dtype):
     """Constant rows, zeros, the smallest and largest values, Inf and NaN in one group of four."""
