@@ -634,6 +634,30 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                         }
                     }
                 }
+                const uint32_t scales = src + Sh::SOFF + TK * 16;
+                uint2 sl[SUB], sh[SUB];                           // 4 bits, values: (NARROW: of this lane's group alone, rows g and g + 8 side by side)
+                uint32_t big = 0;
+                if (BITS == 4) {
+#pragma unroll
+                    for (int u = 0; u < SUB; ++u) {
+                        sl[u] = sh[u] = make_uint2(0u, 0u);
+                        const bool has = u == 0 || key0 + 16 * u < cur.klen;           // (else nothing was copied there)
+                        const uint32_t sc = scales + (u * 16 + kap) * 16;
+                        if constexpr (NARROW) {
+                            if (has) {
+                                sl[u].x = __byte_perm(lds16(sc + 2 * t), lds16(sc + 128 + 2 * t), 0x5410);
+                                sh[u].x = __byte_perm(lds16(sc + 8 + 2 * t), lds16(sc + 136 + 2 * t), 0x5410);             // zero points
+                            }
+                        } else {
+                            const uint2 a = lds64(sc), b = lds64(sc + 128);
+                            if (has) {
+                                sl[u] = a;
+                                sh[u] = b;
+                            }
+                        }
+                        big = __vmaxu2(big, NARROW ? sl[u].x : __vmaxu2(__vmaxu2(sl[u].x, sl[u].y), __vmaxu2(sh[u].x, sh[u].y)));     // (scales are not negative)
+                    }
+                }
                 // ---- bias, mask, reference (raw scores) ------------------------------------------------------------------------------
                 if constexpr (BIAS) {
 #pragma unroll
@@ -724,24 +748,6 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                 } else {
                     // The values' scales go into the weights, in fp32 before their one rounding; the codes stay exact.  A weight times a
                     // scale would leave fp16 at either end, so scales are taken relative to a power of two that only grows.
-                    const uint32_t scales = src + Sh::SOFF + TK * 16;
-                    uint2 sl[SUB], sh[SUB];                           // (NARROW: of this lane's group alone, rows g and g + 8 side by side)
-                    uint32_t big = 0;
-#pragma unroll
-                    for (int u = 0; u < SUB; ++u) {
-                        sl[u] = sh[u] = make_uint2(0u, 0u);
-                        if (u == 0 || key0 + 16 * u < cur.klen) {                      // (else nothing was copied there)
-                            const uint32_t sc = scales + (u * 16 + kap) * 16;
-                            if constexpr (NARROW) {
-                                sl[u].x = __byte_perm(lds16(sc + 2 * t), lds16(sc + 128 + 2 * t), 0x5410);
-                                sh[u].x = __byte_perm(lds16(sc + 8 + 2 * t), lds16(sc + 136 + 2 * t), 0x5410);             // zero points
-                            } else {
-                                sl[u] = lds64(sc);
-                                sh[u] = lds64(sc + 128);
-                            }
-                        }
-                        big = __vmaxu2(big, NARROW ? sl[u].x : __vmaxu2(__vmaxu2(sl[u].x, sl[u].y), __vmaxu2(sh[u].x, sh[u].y)));     // (scales are not negative)
-                    }
                     {
                         constexpr uint32_t top_exp = (0x7FFFu >> N::kExpShift) - 1;    // (NaN: as large as a number can be)
                         const int top = (int)min(__reduce_max_sync(0xffffffffu, max(big & 0xFFFFu, big >> 16)) >> N::kExpShift, top_exp);
@@ -761,8 +767,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                     const float unit = __int_as_float((127 + N::kExpBias - vexp) << 23);
 #pragma unroll
                     for (int u = 0; u < SUB; ++u) {
-                        if (u > 0 && key0 + 16 * u >= cur.klen) break;
-                        uint32_t pf[NT][4][2];
+                        uint32_t pf[NT][4][2];                         // (a piece that does not exist has scales of 0, and any codes are finite)
                         if constexpr (NARROW) {
                             const float2 ss = M::unpack(sl[u].x), zz = M::unpack(sh[u].x);
                             const float a = ss.x * unit, b = ss.y * unit;
@@ -792,11 +797,11 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                         // zero points: rows 0-3 of one more product are the groups'
                         {
                             uint32_t a[4] = {0u, 0u, 0u, 0u};
-                            if (g < 4) {
-                                const uint32_t zp = scales + u * 256 + 8 + 2 * g + t * 16;
-                                a[0] = __byte_perm(lds16(zp), lds16(zp + 64), 0x5410);
-                                a[2] = __byte_perm(lds16(zp + 128), lds16(zp + 192), 0x5410);
-                            }
+                            const bool has = g < 4 && (u == 0 || key0 + 16 * u < cur.klen);
+                            const uint32_t zp = scales + u * 256 + 8 + 2 * (g & 3) + t * 16;
+                            const uint32_t z0 = __byte_perm(lds16(zp), lds16(zp + 64), 0x5410), z1 = __byte_perm(lds16(zp + 128), lds16(zp + 192), 0x5410);
+                            a[0] = has ? z0 : 0u;
+                            a[2] = has ? z1 : 0u;
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt)
                                 M::run(zo[nt], a, movmatrix_trans(M::pack(c[u][nt][0], c[u][nt][1])), movmatrix_trans(M::pack(c[u][nt][2], c[u][nt][3])));
