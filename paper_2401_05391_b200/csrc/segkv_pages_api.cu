@@ -55,16 +55,17 @@ int pack_log(const segkv_pages* h, bool slopes) {
 // CTA of its own, and a round of one such item per SM takes r for 128 keys, however many of the rows are real; the warp-level kernel takes
 // u for 128 keys of every tile of 16 columns (8 at head_dim 256), spread over all SMs.  Both go with the keys' number, which only the device
 // knows, so that the ratio decides.  Measured (2560 keys, us, warp-level / tensor cores): head_dim 128, 32 x 4 heads, 2 sequences of 16
-// tokens 20.4 / 31.8, of 64 37.9 / 32.1, of 128 64.0 / 32.2, of 512 207 / 61.8, 16 of 5 39.5 / 33.3, 64 of 4 111 / 64.2; one of 64 at 32768 keys 168 /
-// 346; 32 x 32 heads, 4 of 32 45.6 / 34.1; head_dim 256, 16 x 16, 4 of 64 193 / 52.9; head_dim 64, 32 x 8, 4 of 64 43.9 / 31.6.  4 bits: head_dim 128, 32 x 4
-// heads, 2 of 64 49.6 / 39.5, of 512 293 / 72.4, 16 of 5 41.8 / 39.6, 64 of 2 (16 columns, 4000 keys) 71.5 / 122; head_dim 256 96.5 / 83.2; head_dim 64 61.5 / 34.4.
+// tokens 15.0 / 32.2, of 64 36.5 / 32.5, of 128 62.1 / 32.7, of 512 203 / 47.6, 16 of 5 34.6 / 33.8, 64 of 4 109 / 64.9; one of 64 at 32768 keys 159 /
+// 351; 32 x 32 heads, 4 of 32 39.7 / 34.3; head_dim 256, 16 x 16, 4 of 64 190 / 53.7; head_dim 64, 32 x 8, 4 of 64 42.6 / 30.7.  4 bits: head_dim 128, 32 x 4
+// heads, 2 of 64 48.3 / 39.6, of 512 285 / 72.3, 16 of 5 40.4 / 39.7, 32 of 6 70.5 / 42.1, 64 of 2 (16 columns, 4000 keys) 69.4 / 122; head_dim 256, 16 x 16, 2 of 64
+// 50.5 / 78.8, 4 of 16 29.6 / 83.2; head_dim 64, 32 x 8, 4 of 64 63.9 / 34.3, 64 x 8, 16 of 6 52.8 / 35.7.
 bool many_rows(const segkv_pages* h, int n, int q_len, long long q_stride, int pack) {
     if (q_stride * q_len * 2 >= 1LL << 40) return false;           // (what a map's stride can hold)
     const long long cols = (long long)q_len * h->group, nc = h->head_dim == 256 ? 8 : 16, ctiles = (cols + nc - 1) / nc;
     if (ctiles < 2) return false;
     const long long items = (long long)n * (h->heads >> pack) * ((((long long)q_len << pack) + 127) / 128);
     const int i = h->head_dim == 64 ? 0 : h->head_dim == 128 ? 1 : 2;
-    static const double us[2][3] = {{4.3, 7.0, 18.8}, {6.0, 7.1, 9.4}}, rs[2][3] = {{1550., 1550., 2600.}, {1700., 1900., 4100.}};      // ns; 16, 4 bits
+    static const double us[2][3] = {{4.3, 7.0, 18.8}, {6.0, 7.1, 9.4}}, rs[2][3] = {{1550., 1550., 2600.}, {1700., 1600., 4100.}};      // ns; 16, 4 bits
     const double u = us[h->bits == 4][i], r = rs[h->bits == 4][i];
     return (double)n * h->kv_heads * ctiles * u > (double)((items + h->sm_count - 1) / h->sm_count) * r;
 }
