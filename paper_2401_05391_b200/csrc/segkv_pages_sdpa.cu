@@ -52,6 +52,7 @@ template <typename T> struct Num;
 template <> struct Num<__half> {
     static constexpr float kLift = 6.f;                      // 16-bit rows: weights carry 2^kLift, so that small ones stay normal
     static constexpr int kExpShift = 10, kExpBias = 15;
+    static constexpr uint32_t kInf = 0x7C00u;
     static __device__ __forceinline__ void mma8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
         asm("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%7,%7,%7,%7};"
             : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(b0), "f"(0.f));
@@ -60,6 +61,7 @@ template <> struct Num<__half> {
 template <> struct Num<__nv_bfloat16> {
     static constexpr float kLift = 0.f;
     static constexpr int kExpShift = 7, kExpBias = 127;
+    static constexpr uint32_t kInf = 0x7F80u;
     static __device__ __forceinline__ void mma8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
         asm("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%7,%7,%7,%7};"
             : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(b0), "f"(0.f));
@@ -330,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
     const uint32_t cs_lane = Sh::SOFF + (lane < 16 ? 0 : TK * 16) + (lane & 15) * 16;
     auto copy_tile = [&](const Cursor& c, int stage) {
         const uint32_t dst = ring + stage * Sh::STAGE;
-        const uint32_t head_at = (uint32_t)c.h * head_bytes;
+        const unsigned long long head_at = (unsigned long long)(uint32_t)c.h * head_bytes;
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
             const int key = c.b * KB + warp * TK + 16 * u;
@@ -642,30 +644,6 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                         }
                     }
                 }
-                const uint32_t scales = src + Sh::SOFF + TK * 16;
-                uint2 sl[SUB], sh[SUB];                           // 4 bits, values: (NARROW: of this lane's group alone, rows g and g + 8 side by side)
-                uint32_t big = 0;
-                if (BITS == 4) {
-#pragma unroll
-                    for (int u = 0; u < SUB; ++u) {
-                        sl[u] = sh[u] = make_uint2(0u, 0u);
-                        const bool has = u == 0 || key0 + 16 * u < cur.klen;           // (else nothing was copied there)
-                        const uint32_t sc = scales + (u * 16 + kap) * 16;
-                        if constexpr (NARROW) {
-                            if (has) {
-                                sl[u].x = __byte_perm(lds16(sc + 2 * t), lds16(sc + 128 + 2 * t), 0x5410);
-                                sh[u].x = __byte_perm(lds16(sc + 8 + 2 * t), lds16(sc + 136 + 2 * t), 0x5410);             // zero points
-                            }
-                        } else {
-                            const uint2 a = lds64(sc), b = lds64(sc + 128);
-                            if (has) {
-                                sl[u] = a;
-                                sh[u] = b;
-                            }
-                        }
-                        big = __vmaxu2(big, NARROW ? sl[u].x : __vmaxu2(__vmaxu2(sl[u].x, sl[u].y), __vmaxu2(sh[u].x, sh[u].y)));     // (scales are not negative)
-                    }
-                }
                 // ---- bias, mask, reference (raw scores) ------------------------------------------------------------------------------
                 if constexpr (BIAS) {
 #pragma unroll
@@ -756,10 +734,47 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
                 } else {
                     // The values' scales go into the weights, in fp32 before their one rounding; the codes stay exact.  A weight times a
                     // scale would leave fp16 at either end, so scales are taken relative to a power of two that only grows.
+                    const uint32_t scales = src + Sh::SOFF + TK * 16;
+                    uint2 sl[SUB], sh[SUB];                           // 4 bits, values: (NARROW: of this lane's group alone, rows g and g + 8 side by side)
+                    uint32_t big = 0;
+#pragma unroll
+                    for (int u = 0; u < SUB; ++u) {
+                        sl[u] = sh[u] = make_uint2(0u, 0u);
+                        const bool has = u == 0 || key0 + 16 * u < cur.klen;           // (else nothing was copied there)
+                        const uint32_t sc = scales + (u * 16 + kap) * 16;
+                        if constexpr (NARROW) {
+                            if (has) {
+                                sl[u].x = __byte_perm(lds16(sc + 2 * t), lds16(sc + 128 + 2 * t), 0x5410);
+                                sh[u].x = __byte_perm(lds16(sc + 8 + 2 * t), lds16(sc + 136 + 2 * t), 0x5410);             // zero points
+                            }
+                        } else {
+                            const uint2 a = lds64(sc), b = lds64(sc + 128);
+                            if (has) {
+                                sl[u] = a;
+                                sh[u] = b;
+                            }
+                        }
+                        big = __vmaxu2(big, NARROW ? sl[u].x : __vmaxu2(__vmaxu2(sl[u].x, sl[u].y), __vmaxu2(sh[u].x, sh[u].y)));     // (scales are not negative)
+                    }
                     {
-                        constexpr uint32_t top_exp = (0x7FFFu >> N::kExpShift) - 1;    // (NaN: as large as a number can be)
-                        const int top = (int)min(__reduce_max_sync(0xffffffffu, max(big & 0xFFFFu, big >> 16)) >> N::kExpShift, top_exp);
-                        if (top > vexp) {
+                        uint32_t most = __reduce_max_sync(0xffffffffu, max(big & 0xFFFFu, big >> 16));
+                        if ((int)(most >> N::kExpShift) > vexp) {
+                            if (most >= N::kInf) {            // a group that is not held is its own affair: its zero point is NaN, its scale here 0
+                                auto held = [](uint32_t w) { return ((w & 0x7FFFu) < N::kInf ? w & 0xFFFFu : 0u) | ((w >> 16 & 0x7FFFu) < N::kInf ? w & 0xFFFF0000u : 0u); };
+                                big = 0;
+#pragma unroll
+                                for (int u = 0; u < SUB; ++u) {
+                                    sl[u].x = held(sl[u].x);
+                                    if (!NARROW) {
+                                        sl[u].y = held(sl[u].y);
+                                        sh[u].x = held(sh[u].x);
+                                        sh[u].y = held(sh[u].y);
+                                    }
+                                    big = __vmaxu2(big, NARROW ? sl[u].x : __vmaxu2(__vmaxu2(sl[u].x, sl[u].y), __vmaxu2(sh[u].x, sh[u].y)));
+                                }
+                                most = __reduce_max_sync(0xffffffffu, max(big & 0xFFFFu, big >> 16));
+                            }
+                            const int top = max((int)(most >> N::kExpShift), vexp);
                             const float down = __int_as_float(max(127 + vexp - top, 0) << 23);
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt)

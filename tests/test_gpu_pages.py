@@ -225,6 +225,25 @@ def test_rows_that_see_nothing_are_zero_whatever_the_values_are(bits, T, lens):
     c.destroy()
 
 
+@pytest.mark.parametrize("heads,T", [(2, 1), (8, 1), (8, 3)])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_a_group_that_is_not_held_leaves_the_others_as_they_are(dtype, heads, T):
+    c, table, n_lens = filled(heads, 2, 128, 16, [60, 200], dtype, 4, 55)
+    q = randn(2, T, heads, 128, dtype=dtype, g=gen(56))
+    clean = c.sdpa(q, table, n_lens)
+    scales = pg.split4(c.v_pages, 16, 128, dtype)[1]
+    for page in (int(table[0, 1]), int(table[1, 7])):
+        scales[page, :, 5, 2] = math.nan                       # scale and zero point of group 2
+        scales[page, :, 5, 6] = math.nan
+    out = c.sdpa(q, table, n_lens)
+    for group in range(4):
+        if group == 2:
+            assert torch.isnan(out[..., group::4]).all()
+        else:
+            assert torch.equal(out[..., group::4], clean[..., group::4])
+    c.destroy()
+
+
 def test_query_rows_of_a_packed_projection():
     c, table, n_lens = filled(8, 2, 64, 16, [33, 90], F16, 16, 61)
     x = randn(2, 3, 8 + 4, 64, dtype=F16, g=gen(62))
