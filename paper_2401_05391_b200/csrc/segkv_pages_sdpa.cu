@@ -53,19 +53,11 @@ template <> struct Num<__half> {
     static constexpr float kLift = 6.f;                      // 16-bit rows: weights carry 2^kLift, so that small ones stay normal
     static constexpr int kExpShift = 10, kExpBias = 15;
     static constexpr uint32_t kInf = 0x7C00u;
-    static __device__ __forceinline__ void mma8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
-        asm("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%7,%7,%7,%7};"
-            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(b0), "f"(0.f));
-    }
 };
 template <> struct Num<__nv_bfloat16> {
     static constexpr float kLift = 0.f;
     static constexpr int kExpShift = 7, kExpBias = 127;
     static constexpr uint32_t kInf = 0x7F80u;
-    static __device__ __forceinline__ void mma8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
-        asm("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%7,%7,%7,%7};"
-            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(b0), "f"(0.f));
-    }
 };
 
 // ---- 4-bit rows: codes as fp16, whatever the dtype ----------------------------------------------------------------------------
