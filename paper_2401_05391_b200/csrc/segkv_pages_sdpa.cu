@@ -5,7 +5,7 @@
 // order, are dealt evenly over a resident grid: every CTA takes one contiguous run of blocks, whatever the lengths
 // are, which only the device knows.  A CTA's run begins and ends inside a work group at most; those two write partial
 // results (maximum, sum, weighted values), and the last CTA to arrive at a work group's counter folds its parts in
-// their order, so that the result does not depend on who is last.
+// their order, so that the result does not depend on who is last.  (Two exceptions, where sharing costs more than it evens out: few groups, short 16-bit ones.)
 //
 // Warps work alone: each copies its own tiles (cp.async, a ring of kStages), scores them with the keys on the M side
 // (S^T[16 keys, 8 columns] = K . Q^T, mma.sync, fp32), keeps its own running reference and sum, and adds
@@ -172,6 +172,16 @@ __device__ __forceinline__ void advance(const Params& p, Cursor& c, int V) {
     if (++c.v < V) enter<NC, KB>(p, c);
 }
 
+// 16 bits: are the runs moved to starts of groups, so that none is shared?  A meeting of CTAs and its fold cost about four and a half
+// blocks.  Moved runs of equal groups hold ceil(groups / G) of them; of unequal ones, half the longest more than the even share or so.  Shared / whole, us, D 128,
+// 64 sequences x 8 kv heads x 100 keys 13.1 / 9.8, x 200 17.4 / 15.1, x 400 24.8 / 22.5, 38 x 8 x 512 (a second round for 8 groups) 19.7 / 21.8, 12 x 32 x 1000 35.7 / 36.6, ragged:
+// 16 x 40 x 500 24.2 / 21.5.  (4 bits, where a block takes twice as long: 64 x 8 x 400 20.7 / 22.2.)
+__device__ __forceinline__ bool whole_groups(unsigned long long total, unsigned long long groups, int longest, int G) {
+    if (longest == 1 || total >= (1u << 28)) return false;    // (no group can be shared; launches of many milliseconds)
+    const unsigned n = (unsigned)groups, g = (unsigned)G, rounds = (n + g - 1) / g;
+    return (unsigned)total == n * (unsigned)longest ? 2 * rounds * (unsigned)longest * g <= 2 * (unsigned)total + 9 * g : longest <= 9;
+}
+
 template <typename T, int D, int NT, int BITS, bool NARROW, bool BIAS>
 __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pages_sdpa_kernel(const __grid_constant__ Params p) {
     using Sh = Shape<D, NT, BITS, NARROW>;
@@ -219,12 +229,12 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
         };
         const int all = __reduce_add_sync(0xffffffffu, nb);
         total = (unsigned long long)all * p.Hkv;
+        const int longest = __reduce_max_sync(0xffffffffu, nb);
         // (quotients by reciprocals: of numbers below 2^19, half a unit off the border)
         auto parts_of = [&](int size) { return (int)(((float)nb + ((float)size - 0.5f)) * (1.f / (float)size)); };
         if ((long long)V * p.Hkv <= G && total < (1u << 19)) {
             const int least = (int)(((float)(unsigned)total + ((float)G - 0.5f)) * (1.f / (float)G));
             // (a part's meeting and fold cost more than a second block: 8 heads x 4 sequences x 100 keys 5.8 -> 4.6, 4 bits x 200 keys 8.3 -> 7.4)
-            const int longest = __reduce_max_sync(0xffffffffu, nb);
             if (longest <= 2) part = longest;
 #pragma unroll 1
             for (int k = 0; k < 4 && !part; ++k)
@@ -238,7 +248,20 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
             if (total < (unsigned long long)G) G = (int)total;      // every CTA of a shared work group has to have a part
             if (cta >= G) return;
             x0 = total * cta / G;
-            blocks = (int)(total * (cta + 1) / G - x0);
+            unsigned long long x1 = total * (cta + 1) / G;
+            if (BITS == 16 && whole_groups(total, (unsigned long long)V * p.Hkv, longest, G)) {
+                auto behind = [&](unsigned long long x) {          // the next start of a group
+                    if (x >= total) return total;
+                    const int at = __ffs(__ballot_sync(0xffffffffu, x < (unsigned long long)incl * p.Hkv)) - 1;
+                    const unsigned size = (unsigned)__shfl_sync(0xffffffffu, nb, at);
+                    const unsigned from = (unsigned)(x - (unsigned long long)(__shfl_sync(0xffffffffu, incl, at) - (int)size) * p.Hkv) % size;
+                    return from ? x + (size - from) : x;
+                };
+                x0 = behind(x0);
+                x1 = behind(x1);
+                if (x0 >= x1) return;
+            }
+            blocks = (int)(x1 - x0);
         }
         const int src = __ffs(__ballot_sync(0xffffffffu, x0 < (unsigned long long)incl * p.Hkv)) - 1;
         const int mine = __shfl_sync(0xffffffffu, units, src), before = __shfl_sync(0xffffffffu, incl, src) - mine;
@@ -254,31 +277,63 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT, BITS, NARROW>::CTAS) pa
         const int per = (V + kThreads - 1) / kThreads;
         long long* s_scan = reinterpret_cast<long long*>(s_merge);
         long long mine = 0;
+        int longest = 0;
         const int v0 = min(tid * per, V), v1 = min(v0 + per, V);
         int klen, nb;
         for (int v = v0; v < v1; ++v) {
             extent<NC, KB>(p, v, &klen, &nb, cta == 0);
             mine += nb;
+            longest = max(longest, nb);
         }
+        longest = __reduce_max_sync(0xffffffffu, longest);
         long long incl = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const long long u = __shfl_up_sync(0xffffffffu, incl, o);
             if (lane >= o) incl += u;
         }
-        if (lane == 31) s_scan[warp] = incl;
+        if (lane == 31) {
+            s_scan[warp] = incl;
+            s_scan[kWarps + warp] = longest;
+        }
         __syncthreads();
         long long before = incl - mine, all = 0;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             if (w < warp) before += s_scan[w];
             all += s_scan[w];
+            longest = max(longest, (int)s_scan[kWarps + w]);
         }
         total = (unsigned long long)all * p.Hkv;
         if (total < (unsigned long long)G) G = (int)total;
         if (cta >= G) return;
         x0 = total * cta / G;
-        blocks = (int)(total * (cta + 1) / G - x0);
+        unsigned long long x1 = total * (cta + 1) / G;
+        if (BITS == 16 && whole_groups(total, (unsigned long long)V * p.Hkv, longest, G)) {                              // (as above)
+            unsigned long long* s_ends = reinterpret_cast<unsigned long long*>(s_scan) + 2 * kWarps;
+            if (tid == 0 && x1 >= total) s_ends[1] = total;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const unsigned long long x = i ? x1 : x0;
+                unsigned long long at = (unsigned long long)before * p.Hkv;
+                if (x < at || x >= at + (unsigned long long)mine * p.Hkv) continue;
+                for (int v = v0;; ++v) {
+                    extent<NC, KB>(p, v, &klen, &nb, false);
+                    const unsigned long long size = (unsigned long long)nb * p.Hkv;
+                    if (x < at + size) {
+                        const unsigned from = (unsigned)(x - at) % (unsigned)nb;
+                        s_ends[i] = from ? x + ((unsigned)nb - from) : x;
+                        break;
+                    }
+                    at += size;
+                }
+            }
+            __syncthreads();
+            x0 = s_ends[0];
+            x1 = s_ends[1];
+            if (x0 >= x1) return;                             // (every thread)
+        }
+        blocks = (int)(x1 - x0);
         unsigned long long at = (unsigned long long)before * p.Hkv;
         if (mine > 0 && x0 >= at && x0 < at + (unsigned long long)mine * p.Hkv) {
             for (int v = v0;; ++v) {

@@ -123,7 +123,8 @@ def test_attention_of_many_rows(shape, dtype, bits):
     (16, F16, 4, 1, 128, 1, [20011]), (4, F16, 2, 2, 128, 1, [3001, 64, 900]), (4, BF16, 1, 1, 256, 1, [8000]), (4, F16, 40, 40, 64, 1, [777] * 9),
     (16, F16, 3, 3, 128, 1, [200 + 37 * i for i in range(40)]), (16, BF16, 80, 80, 64, 1, [500, 0, 1300]), (4, F16, 4, 1, 128, 1, [20011]), (16, BF16, 16, 2, 64, 1, [9999, 3, 70]),
     (4, BF16, 16, 2, 256, 1, [5000, 12000]), (4, F16, 9, 1, 64, 2, [30001]), (16, F16, 2, 2, 256, 1, [7777]),
-    (4, BF16, 8, 1, 128, 4, [4097] * 3)])
+    (4, BF16, 8, 1, 128, 4, [4097] * 3), (16, F16, 32, 8, 128, 1, [200] * 64), (16, BF16, 24, 24, 64, 2, [13 * i for i in range(50)]),
+    (16, F16, 40, 40, 128, 1, [70 * i for i in range(8)]), (16, F16, 16, 16, 256, 1, [250] * 19), (16, BF16, 8, 8, 128, 1, [1, 0] * 40)])
 def test_work_groups_shared_by_many_ctas(bits, dtype, H, Hkv, D, T, lens):
     c, table, n_lens = filled(H, Hkv, D, 64, lens, dtype, bits, 900 + D)
     q = randn(len(lens), T, H, D, dtype=dtype, g=gen(901))

@@ -116,6 +116,28 @@ def test_parts_of_few_work_groups_fit_the_grid(seed):
     assert len(taken) == total
 
 
+@pytest.mark.parametrize("seed", range(20))
+def test_runs_moved_to_starts_of_groups_share_none(seed):
+    """Short 16-bit groups: a run's ends move to the next start of a group; all groups are taken once, whole."""
+    rng = np.random.default_rng(200 + seed)
+    grid, heads = int(rng.choice([148, 296])), int(rng.integers(1, 20))
+    nbs = [int(x) for x in rng.integers(1, 10, size=int(rng.integers(1, 80)))]
+    starts = np.concatenate([[0], np.cumsum(np.repeat(nbs, heads))])
+    total = int(starts[-1])
+    G = min(grid, total)
+
+    def behind(x):
+        return int(starts[np.searchsorted(starts, x)])
+    taken = []
+    for cta in range(G):
+        x0, x1 = behind(total * cta // G), behind(total * (cta + 1) // G)
+        assert x0 <= x1 and x0 in starts and x1 in starts
+        assert x1 - x0 <= total / G + max(nbs)
+        taken.append((x0, x1))
+    assert taken[0][0] == 0 and taken[-1][1] == total
+    assert all(a[1] == b[0] for a, b in zip(taken, taken[1:]))
+
+
 def test_quotients_by_reciprocals_are_right_below_2_to_the_19():
     rng = np.random.default_rng(7)
     for size in [1, 2, 3, 5, 7, 9, 13, 100, 1771, 4097, 99991, 300007]:
